@@ -15,7 +15,7 @@ image at once (forked sequences that share their prompt's pages).
 The 4-bit format, for 32 consecutive values x of one head's key or value (all
 steps in float32, each rounded once):
 
-    x   = min(max(x, -65504), 65504)
+    x   = min(max(x, -61440), 61440)          (so that z + s c stays within f16)
     z   = f16(min x),  s = f16((max x - min x) * f32(1 / 15))
     c_i = min(max(round_half_even((x_i - z) / s), 0), 15), 0 where s = 0
     the value that is held: z + s c_i
@@ -32,7 +32,7 @@ own = False
 DEV = "cuda"
 DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 GROUP = 32                       # values that share a scale and a zero point
-F16_MAX = 65504.0
+LIMIT = 61440.0
 
 
 # ---------------------------------------------------------------- cases
@@ -427,7 +427,7 @@ def _plain_prompt(st):
 
 def _quantised(x):
     """Codes, scales and zero points of x [tokens][heads][head_dim]."""
-    x = x.float().clamp(-F16_MAX, F16_MAX).unflatten(-1, (-1, GROUP))
+    x = x.float().clamp(-LIMIT, LIMIT).unflatten(-1, (-1, GROUP))
     lo, hi = x.amin(-1, keepdim=True), x.amax(-1, keepdim=True)
     z = lo.half()
     s = ((hi - lo) * torch.tensor(1.0 / 15.0, device=x.device)).half()
@@ -557,7 +557,7 @@ def _attend(q, k, v, first):
 def _held(x):
     """The values that the 4-bit format holds for x: its scale, zero point and codes are defined in 16 and 32
     bits, their sum is exact in 64."""
-    y = torch.clip(x.to(torch.float32), -F16_MAX, F16_MAX).reshape(*x.shape[:-1], x.shape[-1] // GROUP, GROUP)
+    y = torch.clip(x.to(torch.float32), -LIMIT, LIMIT).reshape(*x.shape[:-1], x.shape[-1] // GROUP, GROUP)
     low, high = torch.aminmax(y, dim=-1, keepdim=True)
     zero, fifteenth = low.to(torch.float16).to(torch.float32), torch.full_like(low, 1.0 / 15.0)
     step = ((high - low) * fifteenth).to(torch.float16).to(torch.float32)
