@@ -369,6 +369,164 @@ int ios_run_timed(ios_graph *g, ios_schedule_t *q, const float *const *d_inputs,
  * Errors: IOS_E_ARG, IOS_E_HIP. */
 int ios_device_status(ios_graph *g, void *hip_stream, int32_t *flags);
 
+/* ------------------------------------- attention and its key-value cache */
+/* Operators of a token decoder that reads what a CNN trunk saw: attention over
+ * whole prompts, a paged cache that holds keys and values in 4 bits, single
+ * token attention over that cache, and the bookkeeping of its pages.  They
+ * take no graph: every buffer is the caller's, on the current HIP device, and
+ * what changes from call to call (lengths, page tables) stays in device
+ * memory, so that a recorded call can be replayed on other lengths.  Every
+ * call is asynchronous on `hip_stream` (a hipStream_t of the current device;
+ * NULL = the default stream), allocates nothing and may be captured into a HIP
+ * graph; ios_cache_status waits.  Calls on one cache, and calls that share a
+ * workspace, must not overlap in time.  The host cannot refuse what only
+ * device memory holds: the kernels pass over slot and page ids out of range
+ * and clip offsets to the tensors they index.
+ *
+ * Element types.  Sums, softmax statistics and products' accumulators are
+ * float32 whatever the type. */
+enum { IOS_F32 = 0, IOS_F16 = 1, IOS_BF16 = 2 };
+
+/* A [tokens][heads][head_dim] tensor on the device.  Strides count elements
+ * (an input's may be 0); head_dim is contiguous, and `data` and both strides
+ * are multiples of 16 bytes, so that every row starts at one. */
+typedef struct {
+  void *data;
+  int64_t tokens;
+  int64_t token_stride, head_stride;
+} ios_tokens;
+
+/* An attention: o_i = sum_j softmax_j(scale q_i . k_j) v_j, for `heads` heads
+ * of queries, of which heads / kv_heads read each head of keys and values.
+ * A row that sees no key gives 0 (and -infinity as its log-sum-exp). */
+typedef struct {
+  int32_t dtype;             /* IOS_F32 / F16 / BF16, of every tensor of the call      */
+  int32_t heads, kv_heads;   /* heads % kv_heads == 0                                  */
+  int32_t head_dim;          /* prompt: a multiple of 8 up to 128; cache: the cache's  */
+  int32_t seqs;              /* sequences of the call                                  */
+  int32_t causal;            /* prompt: 1 = the last query of a sequence sees its last
+                                key, the one before sees one key less, and so on
+                                (queries may be fewer or more than keys); 0 = all      */
+  int32_t max_keys;          /* no sequence has more keys (0 = unknown); only decides
+                                over how many workgroups a row's keys are spread       */
+  float scale;
+} ios_attn_desc;
+
+/* Bytes of workspace that spreads the keys of few rows over many workgroups,
+ * for q_tokens queries in all.  0: the call uses none.  The workspace needs no
+ * initial values, and nothing in it has to be kept between calls.
+ * Errors: IOS_E_ARG, IOS_E_SHAPE, IOS_E_UNSUPPORTED (as the attention calls). */
+int ios_attn_work_bytes(const ios_attn_desc *d, int64_t q_tokens, int64_t *bytes);
+
+/* Attention over packed prompts: sequence i has queries
+ * cu_q[i] .. cu_q[i+1]-1 of q and out and keys cu_k[i] .. cu_k[i+1]-1 of k and
+ * v (device arrays of seqs + 1 ascending offsets).  lse (float32 [heads]
+ * [q->tokens], or NULL) receives the log-sum-exp of every row's scores, by
+ * which parts of an attention can be joined.  out may not overlap an input;
+ * rows outside every sequence are not written.  A key or value that a row does
+ * not see never changes that row, not even by a NaN.  `work` (of work_bytes)
+ * may be NULL.
+ * Errors: IOS_E_ARG (null pointer, type, sizes, misaligned tensor, workspace
+ * below ios_attn_work_bytes), IOS_E_SHAPE (heads % kv_heads, k and v of
+ * different lengths, q and out of different lengths), IOS_E_UNSUPPORTED
+ * (head_dim), IOS_E_HIP. */
+int ios_attn_prompt(const ios_attn_desc *d, const ios_tokens *q, const ios_tokens *k, const ios_tokens *v,
+                    const ios_tokens *out, float *lse, const int32_t *cu_q, const int32_t *cu_k, void *work,
+                    int64_t work_bytes, void *hip_stream);
+
+/* A paged key-value cache.  A page holds page_tokens consecutive tokens of a
+ * sequence, of every layer and head; a sequence is a slot of the table, which
+ * lists its pages in order; pages can be shared (refs counts the rows that
+ * list a page, 0 = free), and are copied before a sharer writes to one.
+ * Initially refs, lens and the workspace are 0 and the table is -1; the pool
+ * needs no initial values.
+ *
+ * 32 consecutive values x of a head's key or value are held as 4-bit codes c
+ * with a scale s and a zero point z, in float32 arithmetic, each step rounded
+ * to nearest even:
+ *     x = min(max(x, -61440), 61440),   z = f16(min x),
+ *     s = f16((max x - min x) * f32(1/15)),
+ *     c = min(max(rint((x - z) / s), 0), 15), 0 where s = 0;
+ *     the value held is z + s c (within the range of f16).
+ * A NaN among them makes all 32 NaN.  5 bits a value in all. */
+typedef struct {
+  int32_t layers, kv_heads;
+  int32_t head_dim;          /* 32, 64, 96 or 128                                      */
+  int32_t page_tokens;       /* 32, 64, 128 or 256                                     */
+  int32_t pages;             /* pages of the pool                                      */
+  int32_t slots, row;        /* sequences, and pages at most in one                    */
+  void *pool;                /* [layers][pages][ios_cache_page_bytes], 16-byte aligned */
+  int32_t *refs;             /* [pages]                                                */
+  int32_t *table;            /* [slots][row], -1 past a sequence's pages               */
+  int32_t *lens;             /* [slots] tokens                                         */
+  void *work;                /* ios_cache_work_bytes, 16-byte aligned                  */
+} ios_cache;
+
+/* Bytes of one page in one layer, and of the cache's workspace (from the sizes
+ * in *c alone).  Errors: IOS_E_ARG, IOS_E_UNSUPPORTED (head_dim, page_tokens). */
+int ios_cache_page_bytes(const ios_cache *c, int64_t *bytes);
+int ios_cache_work_bytes(const ios_cache *c, int64_t *bytes);
+
+/* Room for add[i] more tokens at the end of sequence seqs[i], i = 0 .. n-1
+ * (device arrays; distinct slots, seqs[i] < 0 or add[i] <= 0 are passed over):
+ * takes the free pages of the lowest ids, in the order of the call, and adds
+ * to lens.  Where a sequence's last page is partly filled and shared, it first
+ * gets a copy of it, in every layer (if every sharer is in the call, the last
+ * one of them keeps the page).  If pages or table entries run out nothing
+ * changes, and ios_cache_status tells.
+ * Errors: IOS_E_ARG, IOS_E_UNSUPPORTED, IOS_E_HIP. */
+int ios_cache_reserve(const ios_cache *c, int32_t n, const int32_t *seqs, const int32_t *add, void *hip_stream);
+
+/* Write keys and values to one layer: tokens cu[i] .. cu[i+1]-1 of k and v
+ * become the last tokens of sequence seqs[i] (after ios_cache_reserve of as
+ * many; where there are more than the sequence has, the first are dropped).
+ * The sequences must be distinct and their pages not shared.
+ * Errors: IOS_E_ARG, IOS_E_SHAPE, IOS_E_UNSUPPORTED, IOS_E_HIP. */
+int ios_cache_append(const ios_cache *c, int32_t layer, int32_t dtype, const ios_tokens *k, const ios_tokens *v,
+                     int32_t n, const int32_t *seqs, const int32_t *cu, void *hip_stream);
+
+/* Read the same tokens back, as the values they are held as (cu[i+1] - cu[i]
+ * = the sequence's length reads all of it; rows for which there is no token
+ * are 0).  Errors: as ios_cache_append. */
+int ios_cache_read(const ios_cache *c, int32_t layer, int32_t dtype, const ios_tokens *k, const ios_tokens *v,
+                   int32_t n, const int32_t *seqs, const int32_t *cu, void *hip_stream);
+
+/* Attention of one query token per sequence, row i of q (d->seqs rows), over
+ * every token that one layer of the cache holds of slot seqs[i] (< 0: none).
+ * lse as ios_attn_prompt, [heads][seqs].
+ * Errors: IOS_E_ARG, IOS_E_SHAPE (sizes that differ from the cache's),
+ * IOS_E_UNSUPPORTED (sizes of the cache), IOS_E_HIP. */
+int ios_attn_cache(const ios_cache *c, int32_t layer, const ios_attn_desc *d, const ios_tokens *q,
+                   const ios_tokens *out, float *lse, const int32_t *seqs, void *work, int64_t work_bytes,
+                   void *hip_stream);
+
+/* children[i] becomes a second sequence with the tokens of parents[i], sharing
+ * its pages (device arrays; children are distinct empty slots, no parent is
+ * also a child; a child that holds tokens is left alone, and ios_cache_status
+ * tells).  Errors: IOS_E_ARG, IOS_E_UNSUPPORTED, IOS_E_HIP. */
+int ios_cache_fork(const ios_cache *c, int32_t n, const int32_t *parents, const int32_t *children, void *hip_stream);
+
+/* Empty the sequences seqs[0 .. n-1]; pages that no other sequence lists
+ * become free.  Errors: IOS_E_ARG, IOS_E_UNSUPPORTED, IOS_E_HIP. */
+int ios_cache_free(const ios_cache *c, int32_t n, const int32_t *seqs, void *hip_stream);
+
+/* Move the pages in use to ids 0 .. *live - 1 (device memory; may be NULL):
+ * the k-th lowest used id at or above that number goes to the k-th lowest free
+ * id below it.  The pool above can then be given to something else.
+ * Errors: IOS_E_ARG, IOS_E_UNSUPPORTED, IOS_E_HIP. */
+int ios_cache_compact(const ios_cache *c, int32_t *live, void *hip_stream);
+
+/* Copy the contents of pages src[i] to dst[i] in every layer (device arrays;
+ * no id is both read and written).  Neither table nor refs change.
+ * Errors: IOS_E_ARG, IOS_E_UNSUPPORTED, IOS_E_HIP. */
+int ios_cache_copy(const ios_cache *c, int32_t n, const int32_t *src, const int32_t *dst, void *hip_stream);
+
+/* Wait for `hip_stream`, read what the calls above could not report, and clear
+ * it: bit 0 = ios_cache_reserve ran out of pages, bit 1 = of table entries,
+ * bit 2 = ios_cache_fork met a child in use.
+ * Errors: IOS_E_ARG, IOS_E_HIP. */
+int ios_cache_status(const ios_cache *c, void *hip_stream, int32_t *flags);
+
 /* Message describing the calling thread's most recent error. */
 const char *ios_last_error(void);
 

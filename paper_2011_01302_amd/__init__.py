@@ -1,5 +1,6 @@
 """Python binding of libios (MI355X-native IOS: inter-operator scheduling and
-stage execution of multi-branch CNN blocks).
+stage execution of multi-branch CNN blocks, and the attention and key-value
+cache operators of a token decoder behind them).
 
 Every function below has the name of the C entry point it wraps (see
 ``include/ios.h``) and only marshals arguments: graph building, the schedule
@@ -43,6 +44,9 @@ IOS_CONV, IOS_SEPCONV, IOS_POOL_MAX, IOS_POOL_AVG, IOS_ADD, IOS_MEAN, IOS_CONCAT
 IOS_CONCURRENT, IOS_MERGE = 0, 1
 IOS_SCHED_DP, IOS_SCHED_SEQUENTIAL, IOS_SCHED_GREEDY = 0, 1, 2
 IOS_CONV_TILE_SHAPES = 20
+IOS_F32, IOS_F16, IOS_BF16 = 0, 1, 2
+# ios_cache_status
+IOS_CACHE_NO_PAGES, IOS_CACHE_NO_ENTRIES, IOS_CACHE_CHILD_USED = 1, 2, 4
 INT64_MAX = (1 << 63) - 1
 
 EXPORTED = ["ios_graph_create", "ios_graph_destroy", "ios_add_input", "ios_add_op",
@@ -53,7 +57,11 @@ EXPORTED = ["ios_graph_create", "ios_graph_destroy", "ios_add_input", "ios_add_o
             "ios_schedule_from_stages", "ios_schedule_get", "ios_schedule_stats",
             "ios_schedule_tune_tiles", "ios_schedule_destroy", "ios_schedule_dump_costs", "ios_run", "ios_run_noalloc",
             "ios_run_timed",
-            "ios_device_status", "ios_last_error"]
+            "ios_device_status",
+            "ios_attn_work_bytes", "ios_attn_prompt", "ios_attn_cache",
+            "ios_cache_page_bytes", "ios_cache_work_bytes", "ios_cache_reserve", "ios_cache_append",
+            "ios_cache_read", "ios_cache_fork", "ios_cache_free", "ios_cache_compact", "ios_cache_copy",
+            "ios_cache_status", "ios_last_error"]
 
 
 class IosError(RuntimeError):
@@ -74,6 +82,24 @@ class ios_sched_opts(ctypes.Structure):
                 ("mode", "r", "s", "strategies", "warmup", "reps", "repeats", "verify_reps")]
 
 
+class ios_tokens(ctypes.Structure):
+    """A [tokens][heads][head_dim] device tensor: address, tokens, and the
+    strides of a token and a head in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("tokens", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class ios_attn_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("dtype", "heads", "kv_heads", "head_dim", "seqs", "causal", "max_keys")] + [("scale", ctypes.c_float)]
+
+
+class ios_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("layers", "kv_heads", "head_dim", "page_tokens", "pages", "slots", "row")] + \
+               [(n, ctypes.c_void_p) for n in ("pool", "refs", "table", "lens", "work")]
+
+
 COST_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64,
                            ctypes.POINTER(ctypes.c_int32), ctypes.c_int32, ctypes.c_int32,
                            ctypes.POINTER(ctypes.c_int64))
@@ -82,6 +108,7 @@ _P = ctypes.c_void_p
 _i32, _i64 = ctypes.c_int32, ctypes.c_int64
 _pi32, _pi64 = ctypes.POINTER(_i32), ctypes.POINTER(_i64)
 _pf = ctypes.POINTER(ctypes.c_float)
+_pt, _pd, _pc = ctypes.POINTER(ios_tokens), ctypes.POINTER(ios_attn_desc), ctypes.POINTER(ios_cache)
 
 _sig = {
     "ios_graph_create": (ctypes.c_int, [_i32, ctypes.POINTER(_P)]),
@@ -112,6 +139,19 @@ _sig = {
     "ios_run_noalloc": (ctypes.c_int, [_P, _P, ctypes.POINTER(_P), ctypes.POINTER(_P), _P]),
     "ios_run_timed": (ctypes.c_int, [_P, _P, ctypes.POINTER(_P), ctypes.POINTER(_P), _P, _pi64]),
     "ios_device_status": (ctypes.c_int, [_P, _P, _pi32]),
+    "ios_attn_work_bytes": (ctypes.c_int, [_pd, _i64, _pi64]),
+    "ios_attn_prompt": (ctypes.c_int, [_pd, _pt, _pt, _pt, _pt, _P, _P, _P, _P, _i64, _P]),
+    "ios_attn_cache": (ctypes.c_int, [_pc, _i32, _pd, _pt, _pt, _P, _P, _P, _i64, _P]),
+    "ios_cache_page_bytes": (ctypes.c_int, [_pc, _pi64]),
+    "ios_cache_work_bytes": (ctypes.c_int, [_pc, _pi64]),
+    "ios_cache_reserve": (ctypes.c_int, [_pc, _i32, _P, _P, _P]),
+    "ios_cache_append": (ctypes.c_int, [_pc, _i32, _i32, _pt, _pt, _i32, _P, _P, _P]),
+    "ios_cache_read": (ctypes.c_int, [_pc, _i32, _i32, _pt, _pt, _i32, _P, _P, _P]),
+    "ios_cache_fork": (ctypes.c_int, [_pc, _i32, _P, _P, _P]),
+    "ios_cache_free": (ctypes.c_int, [_pc, _i32, _P, _P]),
+    "ios_cache_compact": (ctypes.c_int, [_pc, _P, _P]),
+    "ios_cache_copy": (ctypes.c_int, [_pc, _i32, _P, _P, _P]),
+    "ios_cache_status": (ctypes.c_int, [_pc, _P, _pi32]),
     "ios_last_error": (ctypes.c_char_p, []),
 }
 for _name, (_res, _args) in _sig.items():
@@ -325,6 +365,73 @@ def ios_run_timed(g: int, q: int, d_inputs: Sequence[int], d_outputs: Sequence[i
 def ios_device_status(g: int, stream: int = 0) -> int:
     f = _i32()
     _check(_lib.ios_device_status(g, stream or None, ctypes.byref(f)))
+    return f.value
+
+
+# Attention and the key-value cache.  Tensors come as ios_tokens, other device
+# memory as addresses (0 = NULL), streams as in ios_run.
+
+def ios_attn_work_bytes(d: ios_attn_desc, q_tokens: int) -> int:
+    n = _i64()
+    _check(_lib.ios_attn_work_bytes(ctypes.byref(d), q_tokens, ctypes.byref(n)))
+    return n.value
+
+
+def ios_attn_prompt(d: ios_attn_desc, q: ios_tokens, k: ios_tokens, v: ios_tokens, out: ios_tokens, lse: int,
+                    cu_q: int, cu_k: int, work: int = 0, work_bytes: int = 0, stream: int = 0) -> None:
+    _check(_lib.ios_attn_prompt(d, q, k, v, out, lse or None, cu_q, cu_k, work or None, work_bytes, stream or None))
+
+
+def ios_attn_cache(c: ios_cache, layer: int, d: ios_attn_desc, q: ios_tokens, out: ios_tokens, lse: int, seqs: int,
+                   work: int = 0, work_bytes: int = 0, stream: int = 0) -> None:
+    _check(_lib.ios_attn_cache(c, layer, d, q, out, lse or None, seqs, work or None, work_bytes, stream or None))
+
+
+def ios_cache_page_bytes(c: ios_cache) -> int:
+    n = _i64()
+    _check(_lib.ios_cache_page_bytes(ctypes.byref(c), ctypes.byref(n)))
+    return n.value
+
+
+def ios_cache_work_bytes(c: ios_cache) -> int:
+    n = _i64()
+    _check(_lib.ios_cache_work_bytes(ctypes.byref(c), ctypes.byref(n)))
+    return n.value
+
+
+def ios_cache_reserve(c: ios_cache, n: int, seqs: int, add: int, stream: int = 0) -> None:
+    _check(_lib.ios_cache_reserve(c, n, seqs, add, stream or None))
+
+
+def ios_cache_append(c: ios_cache, layer: int, dtype: int, k: ios_tokens, v: ios_tokens, n: int, seqs: int, cu: int,
+                     stream: int = 0) -> None:
+    _check(_lib.ios_cache_append(c, layer, dtype, k, v, n, seqs, cu, stream or None))
+
+
+def ios_cache_read(c: ios_cache, layer: int, dtype: int, k: ios_tokens, v: ios_tokens, n: int, seqs: int, cu: int,
+                   stream: int = 0) -> None:
+    _check(_lib.ios_cache_read(c, layer, dtype, k, v, n, seqs, cu, stream or None))
+
+
+def ios_cache_fork(c: ios_cache, n: int, parents: int, children: int, stream: int = 0) -> None:
+    _check(_lib.ios_cache_fork(c, n, parents, children, stream or None))
+
+
+def ios_cache_free(c: ios_cache, n: int, seqs: int, stream: int = 0) -> None:
+    _check(_lib.ios_cache_free(c, n, seqs, stream or None))
+
+
+def ios_cache_compact(c: ios_cache, live: int = 0, stream: int = 0) -> None:
+    _check(_lib.ios_cache_compact(c, live or None, stream or None))
+
+
+def ios_cache_copy(c: ios_cache, n: int, src: int, dst: int, stream: int = 0) -> None:
+    _check(_lib.ios_cache_copy(c, n, src, dst, stream or None))
+
+
+def ios_cache_status(c: ios_cache, stream: int = 0) -> int:
+    f = _i32()
+    _check(_lib.ios_cache_status(c, stream or None, ctypes.byref(f)))
     return f.value
 
 

@@ -32,7 +32,9 @@ SOURCES = ["stage_kernel_full.hip", "stage_kernel_full_persist.hip", "stage_kern
            "stage_kernel_sepsplit_persist.hip",
            "stage_kernel_pipe.hip", "stage_kernel_pipe_persist.hip", "stage_kernel_light.hip",
            "stage_kernel_light_persist.hip",
-           "noalloc.hip", "pack.hip", "graph.cpp", "sched.cpp", "exec.cpp", "api.cpp", "stage_launch.cpp"]
+           "attn_prompt.hip", "attn_prompt_float.hip", "attn_cache.hip", "cache.hip", "pages.hip",
+           "noalloc.hip", "pack.hip", "graph.cpp", "sched.cpp", "exec.cpp", "api.cpp", "decoder.cpp",
+           "stage_launch.cpp"]
 
 
 def _compile(src: str) -> str:

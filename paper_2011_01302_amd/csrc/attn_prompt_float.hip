@@ -1,0 +1,198 @@
+// Attention over packed prompts in float32 (ios_attn_prompt): the walk of
+// attn_prompt.hip on v_mfma_f32_32x32x2_f32, every number in 32 bits.  Bound by
+// the fp32 matrix rate, an eighth of the 16-bit one, so plain staging of tiles
+// of 32 keys through registers is enough.
+#include "decoder.h"
+
+namespace ios {
+
+namespace {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+constexpr int kBM = 128, kBN = 32;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct PromptArgs {
+  int heads, ratio, dim, seqs, causal;
+  float scale;
+  ios_tokens q, k, v, out;
+  float *lse;
+  const int32_t *cu_q, *cu_k;
+};
+
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attn_prompt_float_kernel(PromptArgs a) {
+  constexpr int CH = DP / 4, DB = DP / 32, PITCH = DP + 4, LOADS = kBN * CH / 256;
+  __shared__ __align__(16) float sk[kBN * PITCH], sv[kBN * PITCH];
+  __shared__ int odd_rows[2][kBN];            // of this tile and the next: waves may be a tile apart
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, l31 = lane & 31;
+
+  const int64_t x = gridDim.x - 1 - blockIdx.x;
+  auto start = [&](int i) { return clip(a.cu_q[i], a.q.tokens) / kBM + i; };
+  const int seq = find_owner(a.seqs, x, start);
+  const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
+  const int lq = (int)(clip(a.cu_q[seq + 1], a.q.tokens) - qa);
+  const int lk = max((int)(clip(a.cu_k[seq + 1], a.k.tokens) - ka), 0);
+  const int64_t tile = x - start(seq);
+  if (tile * kBM >= lq) return;
+  const int q0 = (int)tile * kBM, r0 = q0 + 32 * wave;
+  const int head = blockIdx.y, kvh = head / a.ratio;
+  const int64_t diff = (int64_t)lk - lq;
+  auto last_key = [&](int row) { return a.causal ? (int)min((int64_t)min(row, lq - 1) + diff, (int64_t)lk - 1) : lk - 1; };
+  const int lim = max(last_key(r0 + l31), -1);
+  const int lim_lo = last_key(r0), lim_hi = last_key(r0 + 31);
+  const int tiles = max(last_key(q0 + kBM - 1) + kBN, 0) / kBN;
+
+  // Q: values 8 i + 4 half + e of query l31 (the order in which K's are read)
+  float qf[DP / 2];
+  const float mul = fmaxf(__builtin_fabsf(a.scale) * kLog2e, 1e-30f), sign = a.scale < 0.f ? -1.f : 1.f;
+  {
+    const float *src = (const float *)a.q.data + (qa + min(r0 + l31, lq - 1)) * a.q.token_stride + head * a.q.head_stride;
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) {
+      const int d = 8 * i + 4 * half;
+      floatx4 w = {0.f, 0.f, 0.f, 0.f};
+      if (d < a.dim) w = *(const floatx4 *)(src + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) qf[4 * i + e] = w[e] * sign;
+    }
+  }
+  const float *kbase = (const float *)a.k.data + ka * a.k.token_stride + kvh * a.k.head_stride;
+  const float *vbase = (const float *)a.v.data + ka * a.v.token_stride + kvh * a.v.head_stride;
+
+  float m = -INFINITY, l = 0.f;
+  floatx16 o[DB];
+  const floatx16 zero = {};
+#pragma unroll
+  for (int i = 0; i < DB; ++i) o[i] = zero;
+
+  floatx4 nk[LOADS], nv[LOADS];                              // the next tile, on its way
+  auto load = [&](int t) {
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) {
+      const int s = p * 256 + tid, r = s / CH, d = s % CH * 4;
+      nk[p] = nv[p] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (t * kBN + r < lk && d < a.dim) {
+        nk[p] = *(const floatx4 *)(kbase + (int64_t)(t * kBN + r) * a.k.token_stride + d);
+        nv[p] = *(const floatx4 *)(vbase + (int64_t)(t * kBN + r) * a.v.token_stride + d);
+      }
+    }
+  };
+  if (tiles > 0) load(0);
+  for (int t = 0; t < tiles; ++t) {
+    int *odd_row = odd_rows[t & 1];
+    if (tid < kBN) odd_row[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) {
+      const int s = p * 256 + tid, r = s / CH, d = s % CH * 4;
+      *(floatx4 *)(sk + r * PITCH + d) = nk[p];
+      *(floatx4 *)(sv + r * PITCH + d) = nv[p];
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= !(__builtin_fabsf(nv[p][e]) < INFINITY);
+      if (odd) odd_row[r] = 1;
+    }
+    __syncthreads();
+    if (t + 1 < tiles) load(t + 1);
+    if (t * kBN > lim_hi) continue;
+    floatx16 s = zero;
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) {
+      const floatx4 kf = *(const floatx4 *)(sk + l31 * PITCH + 8 * i + 4 * half);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[4 * i + e], s, 0, 0, 0);
+    }
+    const bool masked = t * kBN + kBN - 1 > lim_lo;
+    if (masked) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (t * kBN + (r & 3) + 8 * (r >> 2) + 4 * half > lim) s[r] = -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * mul;
+    if (__any(mx > m)) {
+      const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i] *= f;
+    }
+    const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, -mu));
+      l += s[r];
+    }
+    // Infinities and NaN of a key that only some rows see are kept out of the product (0 times one of them is a NaN)
+    // and added where they are seen.
+    const bool odd = masked && __any(odd_row[l31]);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = (r & 3) + 8 * (r >> 2) + 4 * half;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        float vf = sv[key * PITCH + 32 * i + l31];
+        if (odd) vf = __builtin_fabsf(vf) < INFINITY ? vf : 0.f;
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[r], o[i], 0, 0, 0);
+      }
+    }
+    if (odd) {
+      for (int key = 0; key < kBN; ++key) {
+        if (!__builtin_amdgcn_readfirstlane(odd_row[key])) continue;
+        const bool seen = t * kBN + key <= lim;
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float vf = sv[key * PITCH + 32 * i + (r & 3) + 8 * (r >> 2) + 4 * half];
+            if (seen && !(__builtin_fabsf(vf) < INFINITY)) o[i][r] += vf;
+          }
+      }
+    }
+  }
+
+  l += __shfl_xor(l, 32);
+  const int row = r0 + l31;
+  if (row >= lq) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  float *dst = (float *)a.out.data + (qa + row) * a.out.token_stride + head * a.out.head_stride;
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int d = 32 * i + 8 * r4 + 4 * half;
+      if (d < a.dim) {
+        floatx4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = o[i][4 * r4 + e] * inv;
+        *(floatx4 *)(dst + d) = w;
+      }
+    }
+  if (a.lse && half == 0) a.lse[(int64_t)head * a.q.tokens + qa + row] = (m + __builtin_log2f(l)) * kLn2;
+}
+
+template <int DP>
+hipError_t run(const PromptArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((attn_prompt_float_kernel<DP>), dim3((unsigned)(a.q.tokens / kBM + a.seqs), a.heads), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_prompt_float(const ios_attn_desc &d, const ios_tokens &q, const ios_tokens &k,
+                                    const ios_tokens &v, const ios_tokens &out, float *lse, const int32_t *cu_q,
+                                    const int32_t *cu_k, hipStream_t s) {
+  const PromptArgs a{d.heads, d.heads / d.kv_heads, d.head_dim, d.seqs, d.causal, d.scale, q, k, v, out, lse, cu_q, cu_k};
+  if (a.dim <= 32) return run<32>(a, s);
+  if (a.dim <= 64) return run<64>(a, s);
+  if (a.dim <= 96) return run<96>(a, s);
+  return run<128>(a, s);
+}
+
+}  // namespace ios

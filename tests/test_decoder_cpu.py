@@ -1,0 +1,150 @@
+"""Refusals of the decoder operators (attention, 4-bit key-value cache): every
+argument that the host can see is checked before any device work, so these run
+without a GPU."""
+import numpy as np
+import pytest
+
+import paper_2011_01302_amd as I
+
+P = 1 << 20            # a non-null, aligned address that is never touched
+
+
+def desc(**kw):
+    d = I.ios_attn_desc()
+    d.dtype, d.heads, d.kv_heads, d.head_dim, d.seqs, d.causal, d.max_keys, d.scale = I.IOS_BF16, 8, 2, 64, 2, 1, 0, 0.125
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def toks(heads=8, dim=64, n=10, data=P, ts=None, hs=None):
+    return I.ios_tokens(data, n, heads * dim if ts is None else ts, dim if hs is None else hs)
+
+
+def cache(**kw):
+    c = I.ios_cache()
+    c.layers, c.kv_heads, c.head_dim, c.page_tokens, c.pages, c.slots, c.row = 2, 2, 64, 32, 10, 4, 5
+    c.pool = c.refs = c.table = c.lens = c.work = P
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def refused(name, f, *a):
+    with pytest.raises(I.IosError) as e:
+        f(*a)
+    assert e.value.name == name, e.value
+    assert str(e.value)
+
+
+@pytest.mark.parametrize("name,kw", [
+    ("IOS_E_ARG", dict(dtype=3)), ("IOS_E_ARG", dict(dtype=-1)), ("IOS_E_ARG", dict(heads=0)),
+    ("IOS_E_ARG", dict(kv_heads=0)), ("IOS_E_SHAPE", dict(heads=9)), ("IOS_E_UNSUPPORTED", dict(head_dim=60)),
+    ("IOS_E_UNSUPPORTED", dict(head_dim=136)), ("IOS_E_ARG", dict(head_dim=0)), ("IOS_E_ARG", dict(seqs=0)),
+    ("IOS_E_ARG", dict(seqs=65536)), ("IOS_E_ARG", dict(causal=2)), ("IOS_E_ARG", dict(max_keys=-1))])
+def test_attention_descriptor(name, kw):
+    d = desc(**kw)
+    refused(name, I.ios_attn_work_bytes, d, 10)
+    refused(name, I.ios_attn_prompt, d, toks(), toks(2), toks(2), toks(), 0, P, P)
+
+
+def test_prompt_tensors():
+    d = desc()
+    ok = dict(q=toks(), k=toks(2), v=toks(2), out=toks())
+
+    def call(lse=0, cu_q=P, cu_k=P, **kw):
+        a = {**ok, **kw}
+        I.ios_attn_prompt(d, a["q"], a["k"], a["v"], a["out"], lse, cu_q, cu_k)
+    for t in ("q", "k", "v", "out"):
+        refused("IOS_E_ARG", lambda t=t: call(**{t: toks(data=0)}))
+        refused("IOS_E_ARG", lambda t=t: call(**{t: toks(data=P + 8)}))
+        refused("IOS_E_ARG", lambda t=t: call(**{t: toks(ts=516)}))
+        refused("IOS_E_ARG", lambda t=t: call(**{t: toks(hs=68)}))
+        refused("IOS_E_ARG", lambda t=t: call(**{t: toks(ts=-512)}))
+        refused("IOS_E_ARG", lambda t=t: call(**{t: toks(n=-1)}))
+        refused("IOS_E_ARG", lambda t=t: call(**{t: toks(ts=1 << 30)}))
+        refused("IOS_E_ARG", lambda t=t: call(**{t: None}))
+    refused("IOS_E_SHAPE", lambda: call(v=toks(2, n=11)))
+    refused("IOS_E_SHAPE", lambda: call(out=toks(n=11)))
+    refused("IOS_E_ARG", lambda: call(out=toks(ts=0)))
+    refused("IOS_E_ARG", lambda: call(out=toks(hs=0)))
+    refused("IOS_E_ARG", lambda: call(cu_q=0))
+    refused("IOS_E_ARG", lambda: call(cu_k=0))
+    call(q=toks(n=0), out=toks(n=0))          # nothing to do, nothing launched
+    # float32 rows of 4 elements are 16 bytes
+    d.dtype = I.IOS_F32
+    refused("IOS_E_ARG", lambda: call(q=toks(ts=514)))
+
+
+def test_single_token_attention():
+    c, d = cache(), desc()
+    q = toks(n=2)
+
+    def call(c=c, layer=0, d=d, q=q, out=q, seqs=P, work=0, wb=0):
+        I.ios_attn_cache(c, layer, d, q, out, 0, seqs, work, wb)
+    refused("IOS_E_SHAPE", lambda: call(d=desc(kv_heads=4)))
+    refused("IOS_E_SHAPE", lambda: call(d=desc(head_dim=32)))
+    refused("IOS_E_SHAPE", lambda: call(q=toks(n=3)))
+    refused("IOS_E_SHAPE", lambda: call(out=toks(n=1)))
+    refused("IOS_E_ARG", lambda: call(layer=2))
+    refused("IOS_E_ARG", lambda: call(layer=-1))
+    refused("IOS_E_ARG", lambda: call(seqs=0))
+    refused("IOS_E_ARG", lambda: call(c=cache(pool=0)))
+    one = desc(seqs=1, max_keys=1 << 17)
+    need = I.ios_attn_work_bytes(one, 1)
+    assert need > 0                            # few rows, many keys: the work is spread
+    refused("IOS_E_ARG", lambda: call(d=one, q=toks(n=1), out=toks(n=1), work=P, wb=need - 1))
+    refused("IOS_E_ARG", lambda: call(d=one, q=toks(n=1), out=toks(n=1), work=P + 4, wb=need))
+
+
+@pytest.mark.parametrize("name,kw", [
+    ("IOS_E_ARG", dict(layers=0)), ("IOS_E_ARG", dict(kv_heads=0)), ("IOS_E_ARG", dict(pages=0)),
+    ("IOS_E_ARG", dict(slots=0)), ("IOS_E_ARG", dict(row=0)), ("IOS_E_UNSUPPORTED", dict(head_dim=48)),
+    ("IOS_E_UNSUPPORTED", dict(head_dim=160)), ("IOS_E_UNSUPPORTED", dict(page_tokens=16)),
+    ("IOS_E_UNSUPPORTED", dict(page_tokens=96)), ("IOS_E_UNSUPPORTED", dict(slots=1 << 22, row=1 << 10))])
+def test_cache_sizes(name, kw):
+    c = cache(**kw)
+    for f, a in ((I.ios_cache_page_bytes, ()), (I.ios_cache_work_bytes, ()), (I.ios_cache_reserve, (1, P, P)),
+                 (I.ios_cache_append, (0, I.IOS_F16, toks(2), toks(2), 1, P, P)),
+                 (I.ios_cache_read, (0, I.IOS_F16, toks(2), toks(2), 1, P, P)),
+                 (I.ios_cache_fork, (1, P, P)), (I.ios_cache_free, (1, P)), (I.ios_cache_compact, ()),
+                 (I.ios_cache_copy, (1, P, P)), (I.ios_cache_status, ())):
+        refused(name, f, c, *a)
+
+
+def test_cache_calls():
+    c = cache()
+    for f, a in ((I.ios_cache_reserve, (P, P)), (I.ios_cache_fork, (P, P)), (I.ios_cache_free, (P,)),
+                 (I.ios_cache_copy, (P, P))):
+        refused("IOS_E_ARG", f, c, -1, *a)
+        refused("IOS_E_ARG", f, c, 11, *a)
+        refused("IOS_E_ARG", f, c, 1, *([0] * len(a)))
+        f(c, 0, *a)                            # nothing to do
+    for f in (I.ios_cache_append, I.ios_cache_read):
+        refused("IOS_E_ARG", f, c, 2, I.IOS_F16, toks(2), toks(2), 1, P, P)
+        refused("IOS_E_ARG", f, c, 0, 7, toks(2), toks(2), 1, P, P)
+        refused("IOS_E_SHAPE", f, c, 0, I.IOS_F16, toks(2), toks(2, n=9), 1, P, P)
+        refused("IOS_E_ARG", f, c, 0, I.IOS_F16, toks(2, ts=4), toks(2), 1, P, P)
+        refused("IOS_E_ARG", f, c, 0, I.IOS_F16, toks(2), toks(2), 1, 0, P)
+        refused("IOS_E_ARG", f, c, 0, I.IOS_F16, toks(2), toks(2), 5, P, P)
+        f(c, 0, I.IOS_F16, toks(2, n=0), toks(2, n=0), 1, P, P)
+    refused("IOS_E_ARG", I.ios_cache_read, c, 0, I.IOS_F16, toks(2, ts=0), toks(2), 1, P, P)
+    for field in ("pool", "refs", "table", "lens", "work"):
+        refused("IOS_E_ARG", I.ios_cache_compact, cache(**{field: 0}))
+    refused("IOS_E_ARG", I.ios_cache_compact, cache(work=P + 4))
+
+
+def test_cache_bytes():
+    """4 bits a value, and a scale and a zero point of 16 bits for every 32: 5 bits a value."""
+    for dim in (32, 64, 96, 128):
+        for page in (32, 64, 128, 256):
+            c = cache(head_dim=dim, page_tokens=page, kv_heads=3)
+            assert I.ios_cache_page_bytes(c) == 3 * page * 2 * dim * 5 // 8
+    assert I.ios_cache_work_bytes(cache()) >= 4 * 2 * 10
+
+
+def test_work_bytes_depend_on_the_sizes_only():
+    d = desc(seqs=64, max_keys=100)
+    assert I.ios_attn_work_bytes(d, 64) == I.ios_attn_work_bytes(d, 64)
+    assert I.ios_attn_work_bytes(desc(seqs=1, max_keys=64), 1) == 0
+    assert np.all([I.ios_attn_work_bytes(desc(seqs=1, max_keys=m), 1) >= 0 for m in range(0, 5000, 37)])
