@@ -4,7 +4,7 @@
 // for each of its queries: bound by memory, if the 4-bit codes become operands
 // of the matrix instruction with few instructions.  A workgroup takes up to 16
 // queries that share a head of keys (one column of the product each) and a
-// range of the sequence; its four waves take tiles of 32 keys in turn and are
+// range of the sequence; its eight waves take tiles of 32 keys in turn and are
 // joined at the end, the ranges in a second launch.
 //
 // Scores are exact up to 32-bit sums: with q summed over the values of a
@@ -24,14 +24,35 @@ namespace ios {
 namespace {
 
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
-typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bfx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bfx8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kCols = 16;                // queries (heads of one key head) of a workgroup
-constexpr int kWavesA = 4;
+constexpr int kWavesA = 8, kThreadsA = 64 * kWavesA;
+constexpr int kStages = 2;               // tiles of a wave's ring
+constexpr int kMaxSplits = 512, kWantBlocks = 1024, kMinKeys = 512;
+typedef __attribute__((address_space(3))) void lds_void;
+// one tile in the ring, whole 1024-byte loads
+constexpr int stage_loads(int g) { return (tile_bytes(g) + 1023) / 1024; }
+constexpr int stage_bytes(int g) { return stage_loads(g) * 1024; }
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "vmcnt is 6 bits");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// Copy a tile to LDS, 16 bytes a lane and load, through no register (the compiler does not see the write); what is
+// past `bytes` reads as 0.
+template <int G>
+__device__ __forceinline__ void copy_tile(const unsigned char *tile, unsigned char *lds, int lane) {
+  const __amdgpu_buffer_rsrc_t r =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(tile), (short)0, tile_bytes(G), 0x00020000);
+#pragma unroll
+  for (int i = 0; i < stage_loads(G); ++i)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds + i * 1024), 16, lane * 16 + i * 1024, 0, 0, 0);
+}
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // a row's maximum is only followed when it grows by more than 2^8: p stays below 2^8, sums in 32 bits
 constexpr float kSlack = 8.f;
@@ -40,25 +61,21 @@ constexpr float kSlack = 8.f;
 template <class T> constexpr int kQParts = std::is_same_v<T, float> ? 2 : 1;
 template <class T> constexpr int kPParts = std::is_same_v<T, float> ? 3 : std::is_same_v<T, _Float16> ? 2 : 0;
 
-// 8 codes of a word as exact f16 numbers 0 .. 15, in operand order.
-__device__ __forceinline__ halfx8 codes(uint32_t w) {
-  halfx8 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    // 0x6400 | c is the f16 1024 + c
-    const halfx2 h = __builtin_bit_cast(halfx2, (w >> (4 * i) & 0x000F000Fu) | 0x64006400u) - (_Float16)1024;
-    r[2 * i] = h[0];
-    r[2 * i + 1] = h[1];
-  }
-  return r;
-}
-
-// 8 codes as bf16 numbers, 128 + c (0x4300 | c is the bf16 128 + c) ...
-__device__ __forceinline__ bfx8 codes_128(uint32_t w) {
+// 8 codes of a word in operand order, as the 16-bit numbers 2^k + c that `base` | c is in two halves: one
+// instruction to shift and one to mask and set two codes, if the mask is in a vector register (`mask`).
+__device__ __forceinline__ uintx4 codes_over(uint32_t w, uint32_t mask, uint32_t base) {
   uintx4 r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = (w >> (4 * i) & 0x000F000Fu) | 0x43004300u;
-  return __builtin_bit_cast(bfx8, r);
+  for (int i = 0; i < 4; ++i) r[i] = (w >> (4 * i) & mask) | base;
+  return r;
+}
+// As f16 numbers 0 .. 15 (0x6400 | c is 1024 + c) ...
+__device__ __forceinline__ halfx8 codes(uint32_t w, uint32_t mask) {
+  return __builtin_bit_cast(halfx8, codes_over(w, mask, 0x64006400u)) - (_Float16)1024;
+}
+// ... as bf16 numbers 128 + c ...
+__device__ __forceinline__ bfx8 codes_128(uint32_t w, uint32_t mask) {
+  return __builtin_bit_cast(bfx8, codes_over(w, mask, 0x43004300u));
 }
 // ... or c itself.
 __device__ __forceinline__ bfx8 codes_bf(uint32_t w) {
@@ -66,10 +83,6 @@ __device__ __forceinline__ bfx8 codes_bf(uint32_t w) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)(w >> nibble_shift(e) & 15);
   return r;
-}
-
-__device__ __forceinline__ float half_of(uint32_t w, int hi) {
-  return (float)__builtin_bit_cast(_Float16, (uint16_t)(hi ? w >> 16 : w));
 }
 
 // Maximum and sum over the 4 lanes that hold a column (l, l ^ 16, l ^ 32, l ^ 48).
@@ -83,12 +96,12 @@ __device__ __forceinline__ float col_sum(float v) {
 }
 
 template <class T, int G>
-__global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads, int ratio, float scale, ios_tokens q,
+__global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int heads, int ratio, float scale, ios_tokens q,
                                                          ios_tokens out, float *lse, const int32_t *seqs,
-                                                         float *part) {
+                                                         int chunk, float *part) {
   constexpr int D = 32 * G, NT = 2 * G, VW = v_words(G);
-  __shared__ float red_o[kWavesA][kCols][D + 1];
-  __shared__ float red_ml[kWavesA][2][kCols];
+  constexpr int NL = stage_loads(G), SB = stage_bytes(G), RB = (kWavesA * kCols * (D + 1) + kWavesA * 2 * kCols) * 4;
+  __shared__ __align__(16) unsigned char lds[kWavesA * kStages * SB > RB ? kWavesA * kStages * SB : RB];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, kq = lane >> 4;
   const int split = blockIdx.x, splits = gridDim.x, i = blockIdx.z;
@@ -97,10 +110,13 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
   const int cols = min(ratio - c0, kCols), head0 = kvh * ratio + c0;
   const int slot = seqs[i], len = cache_len(c, slot);
   const int tiles = (len + kTileKeys - 1) / kTileKeys;
-  const int t0 = (int)((int64_t)tiles * split / splits), t1 = (int)((int64_t)tiles * (split + 1) / splits);
+  const int t0 = (int)min((int64_t)split * chunk, (int64_t)tiles);
+  const int t1 = split + 1 == splits ? tiles : min(t0 + chunk, tiles);
+  if (part && t0 >= t1) return;                                   // the parts' count leaves this one out
 
-  // the queries as f16 operands: multiplied by a power of two that brings the row's largest value to 2^14 .. 2^15,
-  // so that bf16 values fit (those below 2^-28 of the largest lose bits); the scores are multiplied back
+  // the queries as f16 operands: multiplied by a power of two that brings the row's largest value to 2^8 .. 2^9 (so
+  // that sums of 32 fit too; values below 2^-22 of the largest lose bits), which the scores are multiplied back by;
+  // the sign of the scale goes into them
   constexpr int QP = kQParts<T>, PP = kPParts<T>;
   halfx8 qf[G][QP];
   float qs[G], mul;
@@ -118,9 +134,10 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
     }
     m = col_max(m);
     const int ex = __builtin_bit_cast(int, m) >> 23;              // biased exponent, 0 .. 255
-    const int sh = ex == 0 || ex == 255 ? 0 : min(14 + 127 - ex, 126);
-    const float up = __builtin_bit_cast(float, (uint32_t)(127 + sh) << 23);
-    mul = scale * kLog2e / up;
+    const int sh = ex == 0 || ex == 255 ? 0 : min(8 + 127 - ex, 126);
+    float up = __builtin_bit_cast(float, (uint32_t)(127 + sh) << 23);
+    mul = fmaxf(__builtin_fabsf(scale) * kLog2e / up, 1e-30f);
+    up = scale < 0.f ? -up : up;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       float s = 0.f;
@@ -137,6 +154,15 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
       qs[g] = col_sum(s);
     }
   }
+  // their sums by group as an operand, in two f16 parts: slot 4 kq + g of the product with a key's zero points
+  halfx4 qz = {0, 0, 0, 0};
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const _Float16 hi = (_Float16)qs[g];
+    qz[g] = kq == 0 ? hi : kq == 1 ? (_Float16)(qs[g] - (float)hi) : (_Float16)0;
+  }
+  uint32_t mask = 0x000F000Fu;
+  asm("" : "+v"(mask));
 
   float m = -INFINITY, l = 0.f;
   floatx4 o[NT];
@@ -144,35 +170,86 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
   for (int t = 0; t < NT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
   float zs[G] = {};                                               // PP > 0: sum of p (z - offset s), this lane's keys
 
-  for (int t = t0 + wave; t < t1; t += kWavesA) {
-    const uint32_t *tile = (const uint32_t *)cache_tile(c, slot, t * kTileKeys, kvh, tile_bytes(G));
-    if (!tile) continue;
-    const int left = len - t * kTileKeys;                         // keys of the tile, when below 32
+  // a ring of kStages tiles per wave: while one is worked on, the others are on their way
+  const int first = t0 + wave, n = first < t1 ? (t1 - first + kWavesA - 1) / kWavesA : 0;
+  unsigned char *ring = lds + wave * (kStages * SB);
+  typedef const __attribute__((address_space(4))) int32_t const_i32;   // read through the scalar cache: the vector
+  const_i32 *pages = (const_i32 *)(c.table + (int64_t)slot * c.row);   // loads' counter is the ring's
+  const int tile_lg = c.page_lg - 5;
+  auto page_of = [&](int k) {
+    const int t = first + k * kWavesA;
+    return t < t1 ? pages[t >> tile_lg] : -1;
+  };
+  uint32_t sound = 0;                                             // bit j: the j-th last tile issued has a page
+  auto issue = [&](int k, int page) {
+    const int t = first + k * kWavesA;
+    const bool ok = (unsigned)page < (unsigned)c.pages;
+    const unsigned char *tile = c.pool + (ok ? page : 0) * c.page_bytes + (int64_t)kvh * c.head_bytes +
+                                (t & ((1 << tile_lg) - 1)) * tile_bytes(G);
+    sound = sound << 1 | (ok ? 1u : 0u);
+    copy_tile<G>(tile, ring + k % kStages * SB, lane);
+  };
+#pragma unroll
+  for (int k = 0; k < kStages - 1; ++k)
+    if (k < n) issue(k, page_of(k));
+  int page = page_of(kStages - 1);
+  for (int k = 0; k < n; ++k) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // the reads of the slot that is loaded next
+    const int ahead = min(kStages - 1, n - 1 - k);                // tiles issued after this one
+    if (k + kStages - 1 < n) {
+      issue(k + kStages - 1, page);
+      page = page_of(k + kStages);
+      wait_loads<NL *(kStages - 1)>();
+    } else if (kStages > 3 && ahead == 2) {
+      wait_loads<NL * 2>();
+    } else if (kStages > 2 && ahead == 1) {
+      wait_loads<NL>();
+    } else {
+      wait_loads<0>();
+    }
+    if (!(sound >> ahead & 1)) continue;
+    const uint32_t *tile = (const uint32_t *)(ring + k % kStages * SB);
+    const int left = len - (first + k * kWavesA) * kTileKeys;     // keys of the tile, when below 32
+    const _Float16 *half = (const _Float16 *)tile;
+    if (left < kTileKeys) {                                       // what is past the last token may be anything
+      for (int x = lane; x < G * kTileKeys; x += 64) {
+        const int key = x & 31;
+        _Float16 *vp = (_Float16 *)const_cast<uint32_t *>(tile + v_param(G, x >> 5, v_quarter(key))) + v_elem(key);
+        if (key >= left) vp[0] = vp[8] = (_Float16)0;
+      }
+    }
     // scores: lane holds keys 16 b + 4 kq + r of query col
-    float s[2][4];
+    floatx4 s[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+      halfx4 kz = {0, 0, 0, 0};
+#pragma unroll
+      for (int g = 0; g < G; ++g) kz[g] = half[k_zero(G, g, 16 * b + col)];
+      s[b] = __builtin_amdgcn_mfma_f32_16x16x16f16(kz, qz, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        const uint32_t w = tile[(b * 64 + lane) * G + g];
-        const halfx8 kc = codes(w);
+        const halfx8 kc = codes(tile[(b * 64 + lane) * G + g], mask);
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < QP; ++k) x = __builtin_amdgcn_mfma_f32_16x16x32_f16(kc, qf[g][k], x, 0, 0, 0);
-        const uintx4 p = *(const uintx4 *)(tile + k_param(G, g, 16 * b + 4 * kq));
+        const halfx4 ks = *(const halfx4 *)(half + k_scale(G, g, 16 * b + 4 * kq));
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          acc[r] = fmaf(half_of(p[r], 0), x[r], fmaf(half_of(p[r], 1), qs[g], acc[r]));
+        for (int r = 0; r < 4; ++r) s[b][r] = fmaf((float)ks[r], x[r], s[b][r]);
       }
+    }
+    if (left < kTileKeys) {
+      asm volatile("");                                           // a branch, not selects in every tile
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[b][r] = 16 * b + 4 * kq + r < left ? acc[r] * mul : -INFINITY;
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[b][r] = 16 * b + 4 * kq + r < left ? s[b][r] : -INFINITY;
     }
     float mx = s[0][0];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[b][r]);
+    mx *= mul;
     if (__any(mx > m + kSlack)) {
       // each row by its own scores alone, so that no row's result depends on another's
       const float rm = col_max(mx), mn = rm > m + kSlack ? rm : m;
@@ -189,18 +266,13 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
     halfx8 ph;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] - mu);
+      p[e] = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], mul, -mu));
       l += p[e];
       ph[e] = (_Float16)p[e];
     }
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      halfx8 vs = *(const halfx8 *)(tile + v_param(G, g, kq)), vz = *(const halfx8 *)(tile + v_param(G, g, kq) + 4);
-      if (left < kTileKeys) {                                     // what is past the last token may be anything
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (4 * kq + (e & 3) + 16 * (e >> 2) >= left) vs[e] = vz[e] = (_Float16)0;
-      }
+      const halfx8 vs = *(const halfx8 *)(tile + v_param(G, g, kq)), vz = *(const halfx8 *)(tile + v_param(G, g, kq) + 4);
       bfx8 pp[PP > 0 ? PP : 1];
       if constexpr (PP > 0) {
         constexpr float offset = PP == 2 ? 128.f : 0.f;
@@ -219,11 +291,11 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
       for (int t2 = 2 * g; t2 < 2 * g + 2; ++t2) {
         const uint32_t w = tile[128 * G + (t2 / VW * 64 + lane) * VW + t2 % VW];
         if constexpr (PP > 0) {
-          const bfx8 vc = PP == 2 ? codes_128(w) : codes_bf(w);
+          const bfx8 vc = PP == 2 ? codes_128(w, mask) : codes_bf(w);
 #pragma unroll
           for (int k = 0; k < PP; ++k) o[t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc, pp[k], o[t2], 0, 0, 0);
         } else {
-          o[t2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes(w) * vs + vz, ph, o[t2], 0, 0, 0);
+          o[t2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes(w, mask) * vs + vz, ph, o[t2], 0, 0, 0);
         }
       }
     }
@@ -239,6 +311,9 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
       o[2 * g + 1] += z;
     }
   }
+  __syncthreads();                                                // the rings are done with
+  auto *red_o = (float(*)[kCols][D + 1])lds;
+  auto *red_ml = (float(*)[2][kCols])(lds + kWavesA * kCols * (D + 1) * 4);
   if (kq == 0) {
     red_ml[wave][0][col] = m;
     red_ml[wave][1][col] = l;
@@ -248,7 +323,7 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
 #pragma unroll
     for (int r = 0; r < 4; ++r) red_o[wave][col][16 * t + 4 * kq + r] = o[t][r];
   __syncthreads();
-  for (int x = threadIdx.x; x < cols * D; x += 256) {
+  for (int x = threadIdx.x; x < cols * D; x += kThreadsA) {
     const int h = x / D, d = x % D;
     float mm = -INFINITY, ll = 0.f, v = 0.f;
 #pragma unroll
@@ -262,11 +337,11 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
     }
     const int64_t row = (int64_t)i * heads + head0 + h;
     if (part) {
-      float *p = part + (row * splits + split) * (D + 2);
-      p[2 + d] = v;
+      part[(row * splits + split) * D + d] = v;
       if (d == 0) {
-        p[0] = mm;
-        p[1] = ll;
+        float *ml = part + (int64_t)q.tokens * heads * splits * D + (row * splits + split) * 2;
+        ml[0] = mm;
+        ml[1] = ll;
       }
     } else {
       ((T *)out.data)[(int64_t)i * out.token_stride + (int64_t)(head0 + h) * out.head_stride + d] =
@@ -276,37 +351,67 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheView c, int heads,
   }
 }
 
-// Join the splits of a row: one workgroup per row, a thread per value.
-template <class T>
-__global__ __launch_bounds__(128) void attn_join_kernel(int heads, int dim, int splits, ios_tokens out, float *lse,
-                                                        const float *part) {
+// Join the parts of a row: one workgroup per row.  Weights of the parts first, then four values a thread, the parts
+// spread over the threads; every sum in a fixed order.
+template <class T, int G>
+__global__ __launch_bounds__(256) void attn_join_kernel(CacheView c, int heads, int splits, int chunk, ios_tokens out,
+                                                        float *lse, const int32_t *seqs, const float *part) {
+  constexpr int D = 32 * G, Q = D / 4, W = 256 / Q;               // W threads share four values
+  __shared__ float weight[kMaxSplits], red[2][4];
+  __shared__ floatx4 sum[W][Q];
   const int64_t row = blockIdx.x, i = row / heads, h = row % heads;
-  const float *p = part + row * splits * (dim + 2);
-  float mm = -INFINITY;
-  for (int s = 0; s < splits; ++s) mm = fmaxf(mm, p[(int64_t)s * (dim + 2)]);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tiles = (cache_len(c, seqs[i]) + kTileKeys - 1) / kTileKeys;
+  const int n = min((tiles + chunk - 1) / chunk, splits);         // parts that hold anything
+  const float *ml = part + (int64_t)out.tokens * heads * splits * D + row * splits * 2;
+  float mm = -INFINITY, ll = 0.f;
+  for (int s = tid; s < n; s += 256) mm = fmaxf(mm, ml[2 * s]);
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) mm = fmaxf(mm, __shfl_xor(mm, x));
+  if (lane == 0) red[0][wave] = mm;
+  __syncthreads();
+  mm = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   const float mu = mm == -INFINITY ? 0.f : mm;
-  float ll = 0.f, v = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const float *ps = p + (int64_t)s * (dim + 2);
-    const float a = __builtin_amdgcn_exp2f(ps[0] - mu);
-    ll = fmaf(a, ps[1], ll);
-    if ((int)threadIdx.x < dim) v = fmaf(a, ps[2 + threadIdx.x], v);
+  for (int s = tid; s < n; s += 256) {
+    weight[s] = __builtin_amdgcn_exp2f(ml[2 * s] - mu);
+    ll = fmaf(weight[s], ml[2 * s + 1], ll);
   }
-  if ((int)threadIdx.x < dim)
-    ((T *)out.data)[i * out.token_stride + h * out.head_stride + threadIdx.x] = (T)(ll == 0.f ? 0.f : v / ll);
-  if (lse && threadIdx.x == 0) lse[h * out.tokens + i] = (mm + __builtin_log2f(ll)) * kLn2;
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) ll += __shfl_xor(ll, x);
+  if (lane == 0) red[1][wave] = ll;
+  __syncthreads();
+  ll = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+  const int d4 = tid % Q, w = tid / Q;
+  floatx4 v = {0.f, 0.f, 0.f, 0.f};
+  if (w < W)
+    for (int s = w; s < n; s += W) v += weight[s] * *(const floatx4 *)(part + (row * splits + s) * D + 4 * d4);
+  if (w < W) sum[w][d4] = v;
+  __syncthreads();
+  if (w == 0) {
+#pragma unroll
+    for (int x = 1; x < W; ++x) v += sum[x][d4];
+    struct alignas(4 * sizeof(T)) { T v[4]; } r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.v[e] = (T)(ll == 0.f ? 0.f : v[e] / ll);
+    *(decltype(r) *)((T *)out.data + i * out.token_stride + h * out.head_stride + 4 * d4) = r;
+  }
+  if (lse && tid == 0) lse[h * out.tokens + i] = (mm + __builtin_log2f(ll)) * kLn2;
 }
+
+int64_t keys_of(const ios_attn_desc &d) { return d.max_keys ? d.max_keys : 1 << 16; }
 
 template <class T, int G>
 hipError_t run(const CacheView &c, const ios_attn_desc &d, const ios_tokens &q, const ios_tokens &out, float *lse,
                const int32_t *seqs, float *part, int splits, hipStream_t s) {
   const int ratio = d.heads / d.kv_heads, blocks = (ratio + kCols - 1) / kCols;
-  hipLaunchKernelGGL((attn_cache_kernel<T, G>), dim3(splits, d.kv_heads * blocks, d.seqs), dim3(64 * kWavesA), 0, s, c,
-                     d.heads, ratio, d.scale, q, out, lse, seqs, splits > 1 ? part : nullptr);
+  // tiles of a part; a sequence longer than max_keys makes its last part longer
+  const int chunk = (int)std::max<int64_t>(1, (keys_of(d) + (int64_t)kTileKeys * splits - 1) / ((int64_t)kTileKeys * splits));
+  hipLaunchKernelGGL((attn_cache_kernel<T, G>), dim3(splits, d.kv_heads * blocks, d.seqs), dim3(kThreadsA), 0, s, c,
+                     d.heads, ratio, d.scale, q, out, lse, seqs, chunk, splits > 1 ? part : nullptr);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
-  hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)((int64_t)d.seqs * d.heads)), dim3(128), 0, s, d.heads,
-                     d.head_dim, splits, out, lse, part);
+  hipLaunchKernelGGL((attn_join_kernel<T, G>), dim3((unsigned)((int64_t)d.seqs * d.heads)), dim3(256), 0, s, c, d.heads,
+                     splits, chunk, out, lse, seqs, part);
   return hipGetLastError();
 }
 
@@ -323,11 +428,13 @@ hipError_t for_groups(const CacheView &c, const ios_attn_desc &d, const ios_toke
 
 }  // namespace
 
+// Parts of a sequence's keys: enough workgroups for the chip (two to a CU at a time), but at least kMinKeys keys
+// each, and no parts (no second launch) where ...
 int cache_splits(const ios_attn_desc &d) {
   const int ratio = d.heads / d.kv_heads;
   const int64_t blocks = (int64_t)d.seqs * d.kv_heads * ((ratio + kCols - 1) / kCols);
-  const int64_t keys = d.max_keys ? d.max_keys : 1 << 16;
-  return (int)std::max<int64_t>(1, std::min((1024 + blocks - 1) / blocks, (keys + 255) / 256));
+  const int64_t parts = std::min<int64_t>((kWantBlocks + blocks - 1) / blocks, keys_of(d) / kMinKeys);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(parts, kMaxSplits));
 }
 
 hipError_t launch_attn_cache(const CacheView &c, const ios_attn_desc &d, const ios_tokens &q, const ios_tokens &out,

@@ -111,7 +111,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, ios_toke
     const Quant b = quantise((const T *)v.data + row * v.token_stride + head * v.head_stride + oct * 8);
     vc[o] = b.word;
     if (q == 0) {
-      img[k_param(G, g, key)] = a.param;
+      ((uint16_t *)img)[k_scale(G, g, key)] = (uint16_t)a.param;
+      ((uint16_t *)img)[k_zero(G, g, key)] = (uint16_t)(a.param >> 16);
       uint16_t *p = (uint16_t *)(img + v_param(G, g, v_quarter(key))) + v_elem(key);
       p[0] = (uint16_t)b.param;
       p[8] = (uint16_t)(b.param >> 16);
@@ -169,7 +170,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, ios_tokens
   for (int o = tid; o < kTileKeys * 4 * G; o += 256) {
     const int key = o / (4 * G), oct = o % (4 * G), g = oct / 4, q = oct % 4;
     if (key < j.lo || key >= j.hi) continue;
-    const uint32_t kw = img[k_word(G, key, q, g)], kp = img[k_param(G, g, key)];
+    const uint16_t *half = (const uint16_t *)img;
+    const uint32_t kw = img[k_word(G, key, q, g)], kp = half[k_scale(G, g, key)] | (uint32_t)half[k_zero(G, g, key)] << 16;
     const uint16_t *p = (const uint16_t *)(img + v_param(G, g, v_quarter(key))) + v_elem(key);
     const uint32_t vp = p[0] | (uint32_t)p[8] << 16;
     Row8<T> kr, vr;

@@ -17,7 +17,8 @@ namespace ios {
 //   V codes    [2G / VW][64 lanes][VW words], VW = 4 (2 where G is odd): word
 //              t, lane l holds value 16 t + l % 16 of keys 4 q .. 4 q + 3 and
 //              16 + 4 q .. + 3, q = l / 16
-//   K params   [G][32 keys] words: s (low half) and z of a key
+//   K scales   [G][32 keys] halves
+//   K zeros    [32 keys][G] halves (z sum(q) is a product of its own)
 //   V params   [G][4 q][8 s, 8 z] halves, in the order of a word's keys
 // A word's element j (0 .. 7) is its nibble j / 2 + 4 (j % 2): (w >> 4 i) &
 // 0x000F000F are elements 2 i and 2 i + 1, one in each half.
@@ -32,7 +33,9 @@ __host__ __device__ constexpr int k_word(int g, int key, int octet, int group) {
 __host__ __device__ constexpr int v_word(int g, int t, int lane) {
   return 128 * g + (t / v_words(g) * 64 + lane) * v_words(g) + t % v_words(g);
 }
-__host__ __device__ constexpr int k_param(int g, int group, int key) { return 256 * g + group * 32 + key; }
+// half offsets of K's parameters, word offset of V's
+__host__ __device__ constexpr int k_scale(int g, int group, int key) { return 512 * g + group * 32 + key; }
+__host__ __device__ constexpr int k_zero(int g, int group, int key) { return 544 * g + key * g + group; }
 __host__ __device__ constexpr int v_param(int g, int group, int q) { return 288 * g + group * 32 + q * 8; }
 // key of a tile -> quarter q and element j of its V words
 __host__ __device__ constexpr int v_quarter(int key) { return (key & 15) >> 2; }
