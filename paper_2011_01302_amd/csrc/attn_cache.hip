@@ -108,11 +108,41 @@ __global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int 
   const int blocks = (ratio + kCols - 1) / kCols;                 // of kCols queries per key head
   const int kvh = blockIdx.y / blocks, c0 = blockIdx.y % blocks * kCols;
   const int cols = min(ratio - c0, kCols), head0 = kvh * ratio + c0;
-  const int slot = seqs[i], len = cache_len(c, slot);
+  // What the first loads depend on is fetched side by side: the length, the pages of the wave's first tiles (through
+  // the scalar cache: the vector loads' counter is the ring's) and the queries.
+  typedef const __attribute__((address_space(4))) int32_t const_i32;
+  const int slot = ((const_i32 *)seqs)[i], at = min(max(slot, 0), c.slots - 1);
+  const int first = split * chunk + wave, tile_lg = c.page_lg - 5;
+  const_i32 *pages = (const_i32 *)(c.table + (int64_t)at * c.row);
+  auto page_of = [&](int k) { return pages[min((first + k * kWavesA) >> tile_lg, c.row - 1)]; };
+  int page[kStages];
+#pragma unroll
+  for (int k = 0; k < kStages; ++k) page[k] = page_of(k);
+  const int held = ((const_i32 *)c.lens)[at];
+  struct alignas(16) Row { T v[8]; } rows[G];
+  const T *src = (const T *)q.data + (int64_t)i * q.token_stride + (int64_t)(head0 + min(col, cols - 1)) * q.head_stride;
+#pragma unroll
+  for (int g = 0; g < G; ++g) rows[g] = *(const Row *)(src + 32 * g + 8 * kq);
+
+  const int len = slot == at ? (int)clip(held, (int64_t)c.row << c.page_lg) : 0;
   const int tiles = (len + kTileKeys - 1) / kTileKeys;
-  const int t0 = (int)min((int64_t)split * chunk, (int64_t)tiles);
-  const int t1 = split + 1 == splits ? tiles : min(t0 + chunk, tiles);
-  if (part && t0 >= t1) return;                                   // the parts' count leaves this one out
+  const int t1 = split + 1 == splits ? tiles : min(split * chunk + chunk, tiles);
+  if (part && split * chunk >= t1) return;                        // the parts' count leaves this one out
+  // a ring of kStages tiles per wave: while one is worked on, the others are on their way
+  const int n = first < t1 ? (t1 - first + kWavesA - 1) / kWavesA : 0;
+  unsigned char *ring = lds + wave * (kStages * SB);
+  uint32_t sound = 0;                                             // bit j: the j-th last tile issued has a page
+  auto issue = [&](int k, int page) {
+    const int t = first + k * kWavesA;
+    const bool ok = (unsigned)page < (unsigned)c.pages;
+    const unsigned char *tile = c.pool + (ok ? page : 0) * c.page_bytes + (int64_t)kvh * c.head_bytes +
+                                (t & ((1 << tile_lg) - 1)) * tile_bytes(G);
+    sound = sound << 1 | (ok ? 1u : 0u);
+    copy_tile<G>(tile, ring + k % kStages * SB, lane);
+  };
+#pragma unroll
+  for (int k = 0; k < kStages - 1; ++k)
+    if (k < n) issue(k, page[k]);
 
   // the queries as f16 operands: multiplied by a power of two that brings the row's largest value to 2^8 .. 2^9 (so
   // that sums of 32 fit too; values below 2^-22 of the largest lose bits), which the scores are multiplied back by;
@@ -122,16 +152,13 @@ __global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int 
   float qs[G], mul;
   {
     float f[G][8], m = 0.f;
-    const T *src = (const T *)q.data + (int64_t)i * q.token_stride + (int64_t)(head0 + min(col, cols - 1)) * q.head_stride;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      struct alignas(16) { T v[8]; } r = *(const decltype(r) *)(src + 32 * g + 8 * kq);
+    for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        f[g][e] = (float)r.v[e];
+        f[g][e] = (float)rows[g].v[e];
         m = fmaxf(m, __builtin_fabsf(f[g][e]));
       }
-    }
     m = col_max(m);
     const int ex = __builtin_bit_cast(int, m) >> 23;              // biased exponent, 0 .. 255
     const int sh = ex == 0 || ex == 255 ? 0 : min(8 + 127 - ex, 126);
@@ -170,35 +197,13 @@ __global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int 
   for (int t = 0; t < NT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
   float zs[G] = {};                                               // PP > 0: sum of p (z - offset s), this lane's keys
 
-  // a ring of kStages tiles per wave: while one is worked on, the others are on their way
-  const int first = t0 + wave, n = first < t1 ? (t1 - first + kWavesA - 1) / kWavesA : 0;
-  unsigned char *ring = lds + wave * (kStages * SB);
-  typedef const __attribute__((address_space(4))) int32_t const_i32;   // read through the scalar cache: the vector
-  const_i32 *pages = (const_i32 *)(c.table + (int64_t)slot * c.row);   // loads' counter is the ring's
-  const int tile_lg = c.page_lg - 5;
-  auto page_of = [&](int k) {
-    const int t = first + k * kWavesA;
-    return t < t1 ? pages[t >> tile_lg] : -1;
-  };
-  uint32_t sound = 0;                                             // bit j: the j-th last tile issued has a page
-  auto issue = [&](int k, int page) {
-    const int t = first + k * kWavesA;
-    const bool ok = (unsigned)page < (unsigned)c.pages;
-    const unsigned char *tile = c.pool + (ok ? page : 0) * c.page_bytes + (int64_t)kvh * c.head_bytes +
-                                (t & ((1 << tile_lg) - 1)) * tile_bytes(G);
-    sound = sound << 1 | (ok ? 1u : 0u);
-    copy_tile<G>(tile, ring + k % kStages * SB, lane);
-  };
-#pragma unroll
-  for (int k = 0; k < kStages - 1; ++k)
-    if (k < n) issue(k, page_of(k));
-  int page = page_of(kStages - 1);
+  int next = page[kStages - 1];
   for (int k = 0; k < n; ++k) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // the reads of the slot that is loaded next
     const int ahead = min(kStages - 1, n - 1 - k);                // tiles issued after this one
     if (k + kStages - 1 < n) {
-      issue(k + kStages - 1, page);
-      page = page_of(k + kStages);
+      issue(k + kStages - 1, next);
+      next = page_of(k + kStages);
       wait_loads<NL *(kStages - 1)>();
     } else if (kStages > 3 && ahead == 2) {
       wait_loads<NL * 2>();
@@ -313,40 +318,42 @@ __global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int 
   }
   __syncthreads();                                                // the rings are done with
   auto *red_o = (float(*)[kCols][D + 1])lds;
-  auto *red_ml = (float(*)[2][kCols])(lds + kWavesA * kCols * (D + 1) * 4);
-  if (kq == 0) {
-    red_ml[wave][0][col] = m;
-    red_ml[wave][1][col] = l;
-  }
+  auto *red_m = (float(*)[kCols])(lds + kWavesA * kCols * (D + 1) * 4);
+  auto *red_l = red_m + kWavesA;
+  if (kq == 0) red_m[wave][col] = m;
+  __syncthreads();
+  float mm = m;
+#pragma unroll
+  for (int w = 0; w < kWavesA; ++w) mm = fmaxf(mm, red_m[w][col]);
+  const float f = mm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm);
+  if (kq == 0) red_l[wave][col] = l * f;
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) red_o[wave][col][16 * t + 4 * kq + r] = o[t][r];
+    for (int r = 0; r < 4; ++r) red_o[wave][col][16 * t + 4 * kq + r] = o[t][r] * f;
   __syncthreads();
+#pragma unroll 1
   for (int x = threadIdx.x; x < cols * D; x += kThreadsA) {
     const int h = x / D, d = x % D;
-    float mm = -INFINITY, ll = 0.f, v = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWavesA; ++w) mm = fmaxf(mm, red_ml[w][0][h]);
-    const float mu = mm == -INFINITY ? 0.f : mm;
+    float ll = 0.f, v = 0.f, top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kWavesA; ++w) {
-      const float a = __builtin_amdgcn_exp2f(red_ml[w][0][h] - mu);
-      ll = fmaf(a, red_ml[w][1][h], ll);
-      v = fmaf(a, red_o[w][h][d], v);
+      top = fmaxf(top, red_m[w][h]);
+      ll += red_l[w][h];
+      v += red_o[w][h][d];
     }
     const int64_t row = (int64_t)i * heads + head0 + h;
     if (part) {
       part[(row * splits + split) * D + d] = v;
       if (d == 0) {
         float *ml = part + (int64_t)q.tokens * heads * splits * D + (row * splits + split) * 2;
-        ml[0] = mm;
+        ml[0] = top;
         ml[1] = ll;
       }
     } else {
       ((T *)out.data)[(int64_t)i * out.token_stride + (int64_t)(head0 + h) * out.head_stride + d] =
           (T)(ll == 0.f ? 0.f : v / ll);
-      if (lse && d == 0) lse[(int64_t)(head0 + h) * q.tokens + i] = (mm + __builtin_log2f(ll)) * kLn2;
+      if (lse && d == 0) lse[(int64_t)(head0 + h) * q.tokens + i] = (top + __builtin_log2f(ll)) * kLn2;
     }
   }
 }
@@ -359,7 +366,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(CacheView c, int heads, 
   constexpr int D = 32 * G, Q = D / 4, W = 256 / Q;               // W threads share four values
   __shared__ float weight[kMaxSplits], red[2][4];
   __shared__ floatx4 sum[W][Q];
-  const int64_t row = blockIdx.x, i = row / heads, h = row % heads;
+  const int64_t row = blockIdx.x, i = blockIdx.x / heads, h = blockIdx.x % heads;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tiles = (cache_len(c, seqs[i]) + kTileKeys - 1) / kTileKeys;
   const int n = min((tiles + chunk - 1) / chunk, splits);         // parts that hold anything
@@ -384,7 +391,13 @@ __global__ __launch_bounds__(256) void attn_join_kernel(CacheView c, int heads, 
   const int d4 = tid % Q, w = tid / Q;
   floatx4 v = {0.f, 0.f, 0.f, 0.f};
   if (w < W)
-    for (int s = w; s < n; s += W) v += weight[s] * *(const floatx4 *)(part + (row * splits + s) * D + 4 * d4);
+    for (int s0 = w; s0 < n; s0 += 8 * W) {                        // eight loads at once
+      floatx4 x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = *(const floatx4 *)(part + (row * splits + min(s0 + u * W, n - 1)) * D + 4 * d4);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v += (s0 + u * W < n ? weight[s0 + u * W] : 0.f) * x[u];
+    }
   if (w < W) sum[w][d4] = v;
   __syncthreads();
   if (w == 0) {
