@@ -32,7 +32,11 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 constexpr int kCols = 16;                // queries (heads of one key head) of a workgroup
 constexpr int kWavesA = 8, kThreadsA = 64 * kWavesA;
 constexpr int kStages = 2;               // tiles of a wave's ring
-constexpr int kMaxSplits = 512, kWantBlocks = 1024, kMinKeys = 512;
+// Parts of a sequence's keys: kWantBlocks workgroups if they fill the chip's 256 CUs twice over (they end at
+// different times: 32 sequences of 8k .. 32k keys took 187 us in parts for 512 workgroups, 180 for 1024, 191 for 2048),
+// at least kMinKeys keys each (a tile for every wave), at most kMaxSplits (131072 keys in 512 parts and their join took
+// 27 us, 20 in 256, 18 in 128), and none (no second launch) below kOneKeys: 785 keys take 11 us in one part, 13 in 3.
+constexpr int kMaxSplits = 128, kWantBlocks = 1024, kMinKeys = 256, kOneKeys = 1024;
 typedef __attribute__((address_space(3))) void lds_void;
 // one tile in the ring, whole 1024-byte loads
 constexpr int stage_loads(int g) { return (tile_bytes(g) + 1023) / 1024; }
@@ -364,45 +368,49 @@ template <class T, int G>
 __global__ __launch_bounds__(256) void attn_join_kernel(CacheView c, int heads, int splits, int chunk, ios_tokens out,
                                                         float *lse, const int32_t *seqs, const float *part) {
   constexpr int D = 32 * G, Q = D / 4, W = 256 / Q;               // W threads share four values
+  static_assert(kMaxSplits <= 256, "a thread per part");
   __shared__ float weight[kMaxSplits], red[2][4];
   __shared__ floatx4 sum[W][Q];
   const int64_t row = blockIdx.x, i = blockIdx.x / heads, h = blockIdx.x % heads;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, d4 = tid % Q, w = tid / Q;
+  // the first loads of values do not wait for the length: parts that hold nothing are left out below
+  const floatx4 *src = (const floatx4 *)(part + row * splits * D) + d4;
+  floatx4 x[8];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = src[(int64_t)min(s0 + u * W, splits - 1) * Q];
+  };
+  load(w);
+  const float *ml = part + (int64_t)out.tokens * heads * splits * D + row * splits * 2;
+  const float m0 = ml[2 * min(tid, splits - 1)], l0 = ml[2 * min(tid, splits - 1) + 1];
   const int tiles = (cache_len(c, seqs[i]) + kTileKeys - 1) / kTileKeys;
   const int n = min((tiles + chunk - 1) / chunk, splits);         // parts that hold anything
-  const float *ml = part + (int64_t)out.tokens * heads * splits * D + row * splits * 2;
-  float mm = -INFINITY, ll = 0.f;
-  for (int s = tid; s < n; s += 256) mm = fmaxf(mm, ml[2 * s]);
+  float mm = tid < n ? m0 : -INFINITY;                            // a thread per part
 #pragma unroll
-  for (int x = 1; x < 64; x <<= 1) mm = fmaxf(mm, __shfl_xor(mm, x));
+  for (int y = 1; y < 64; y <<= 1) mm = fmaxf(mm, __shfl_xor(mm, y));
   if (lane == 0) red[0][wave] = mm;
   __syncthreads();
   mm = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-  const float mu = mm == -INFINITY ? 0.f : mm;
-  for (int s = tid; s < n; s += 256) {
-    weight[s] = __builtin_amdgcn_exp2f(ml[2 * s] - mu);
-    ll = fmaf(weight[s], ml[2 * s + 1], ll);
-  }
+  const float mu = mm == -INFINITY ? 0.f : mm, f = tid < n ? __builtin_amdgcn_exp2f(m0 - mu) : 0.f;
+  float ll = tid < n ? f * l0 : 0.f;
+  if (tid < kMaxSplits) weight[tid] = f;
 #pragma unroll
-  for (int x = 1; x < 64; x <<= 1) ll += __shfl_xor(ll, x);
+  for (int y = 1; y < 64; y <<= 1) ll += __shfl_xor(ll, y);
   if (lane == 0) red[1][wave] = ll;
   __syncthreads();
   ll = red[1][0] + red[1][1] + red[1][2] + red[1][3];
-  const int d4 = tid % Q, w = tid / Q;
   floatx4 v = {0.f, 0.f, 0.f, 0.f};
-  if (w < W)
-    for (int s0 = w; s0 < n; s0 += 8 * W) {                        // eight loads at once
-      floatx4 x[8];
+  for (int s0 = w; s0 < n; s0 += 8 * W) {
+    if (s0 != w) load(s0);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = *(const floatx4 *)(part + (row * splits + min(s0 + u * W, n - 1)) * D + 4 * d4);
-#pragma unroll
-      for (int u = 0; u < 8; ++u) v += (s0 + u * W < n ? weight[s0 + u * W] : 0.f) * x[u];
-    }
+    for (int u = 0; u < 8; ++u)
+      if (s0 + u * W < n) v += weight[s0 + u * W] * x[u];
+  }
   if (w < W) sum[w][d4] = v;
   __syncthreads();
   if (w == 0) {
 #pragma unroll
-    for (int x = 1; x < W; ++x) v += sum[x][d4];
+    for (int y = 1; y < W; ++y) v += sum[y][d4];
     struct alignas(4 * sizeof(T)) { T v[4]; } r;
 #pragma unroll
     for (int e = 0; e < 4; ++e) r.v[e] = (T)(ll == 0.f ? 0.f : v[e] / ll);
@@ -441,11 +449,10 @@ hipError_t for_groups(const CacheView &c, const ios_attn_desc &d, const ios_toke
 
 }  // namespace
 
-// Parts of a sequence's keys: enough workgroups for the chip (two to a CU at a time), but at least kMinKeys keys
-// each, and no parts (no second launch) where ...
 int cache_splits(const ios_attn_desc &d) {
   const int ratio = d.heads / d.kv_heads;
   const int64_t blocks = (int64_t)d.seqs * d.kv_heads * ((ratio + kCols - 1) / kCols);
+  if (keys_of(d) < kOneKeys) return 1;
   const int64_t parts = std::min<int64_t>((kWantBlocks + blocks - 1) / blocks, keys_of(d) / kMinKeys);
   return (int)std::max<int64_t>(1, std::min<int64_t>(parts, kMaxSplits));
 }

@@ -175,6 +175,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(PromptArgs a) {
         }
       }
       if (masked) {
+        asm volatile("");                                    // a branch: selects in every tile took a quarter of the walk
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll

@@ -108,6 +108,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_float_kernel(PromptArgs a)
     }
     const bool masked = t * kBN + kBN - 1 > lim_lo;
     if (masked) {
+      asm volatile("");                                      // a branch, not selects in every tile
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (t * kBN + (r & 3) + 8 * (r >> 2) + 4 * half > lim) s[r] = -INFINITY;
