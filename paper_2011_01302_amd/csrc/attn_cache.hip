@@ -17,7 +17,7 @@
 // in 32 bits.
 #include <type_traits>
 
-#include "decoder.h"
+#include "attn_join.h"
 
 namespace ios {
 
@@ -27,7 +27,6 @@ typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bfx8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kCols = 16;                // queries (heads of one key head) of a workgroup
 constexpr int kWavesA = 8, kThreadsA = 64 * kWavesA;
@@ -36,7 +35,7 @@ constexpr int kStages = 2;               // tiles of a wave's ring
 // different times: 32 sequences of 8k .. 32k keys took 187 us in parts for 512 workgroups, 180 for 1024, 191 for 2048),
 // at least kMinKeys keys each (a tile for every wave), at most kMaxSplits (131072 keys in 512 parts and their join took
 // 27 us, 20 in 256, 18 in 128), and none (no second launch) below kOneKeys: 785 keys take 11 us in one part, 13 in 3.
-constexpr int kMaxSplits = 128, kWantBlocks = 1024, kMinKeys = 256, kOneKeys = 1024;
+constexpr int kMaxSplits = kMaxParts, kWantBlocks = 1024, kMinKeys = 256, kOneKeys = 1024;
 typedef __attribute__((address_space(3))) void lds_void;
 // one tile in the ring, whole 1024-byte loads
 constexpr int stage_loads(int g) { return (tile_bytes(g) + 1023) / 1024; }
@@ -57,9 +56,10 @@ __device__ __forceinline__ void copy_tile(const unsigned char *tile, unsigned ch
   for (int i = 0; i < stage_loads(G); ++i)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds + i * 1024), 16, lane * 16 + i * 1024, 0, 0, 0);
 }
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// a row's maximum is only followed when it grows by more than 2^8: p stays below 2^8, sums in 32 bits
-constexpr float kSlack = 8.f;
+// A row's weights are p = 2^(score - m) with m kTop below the largest score when it was last followed, and m is only
+// followed when a score passes it by kTop + 2: then p is at most 2^15, and f16 holds weights down to 2^-38 of the
+// largest (without kTop those below 2^-25 would be lost, which 10^5 keys together would show).
+constexpr float kTop = 13.f, kSlack = kTop + 2.f;
 
 // How T is computed: parts of q, parts of p s (0: values rounded to f16).
 template <class T> constexpr int kQParts = std::is_same_v<T, float> ? 2 : 1;
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int 
     mx *= mul;
     if (__any(mx > m + kSlack)) {
       // each row by its own scores alone, so that no row's result depends on another's
-      const float rm = col_max(mx), mn = rm > m + kSlack ? rm : m;
+      const float rm = col_max(mx), mn = rm > m + kSlack ? rm - kTop : m;
       const float a = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= a;
@@ -362,61 +362,16 @@ __global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int 
   }
 }
 
-// Join the parts of a row: one workgroup per row.  Weights of the parts first, then four values a thread, the parts
-// spread over the threads; every sum in a fixed order.
 template <class T, int G>
 __global__ __launch_bounds__(256) void attn_join_kernel(CacheView c, int heads, int splits, int chunk, ios_tokens out,
                                                         float *lse, const int32_t *seqs, const float *part) {
-  constexpr int D = 32 * G, Q = D / 4, W = 256 / Q;               // W threads share four values
-  static_assert(kMaxSplits <= 256, "a thread per part");
-  __shared__ float weight[kMaxSplits], red[2][4];
-  __shared__ floatx4 sum[W][Q];
-  const int64_t row = blockIdx.x, i = blockIdx.x / heads, h = blockIdx.x % heads;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, d4 = tid % Q, w = tid / Q;
-  // the first loads of values do not wait for the length: parts that hold nothing are left out below
-  const floatx4 *src = (const floatx4 *)(part + row * splits * D) + d4;
-  floatx4 x[8];
-  auto load = [&](int s0) {
-#pragma unroll
-    for (int u = 0; u < 8; ++u) x[u] = src[(int64_t)min(s0 + u * W, splits - 1) * Q];
-  };
-  load(w);
-  const float *ml = part + (int64_t)out.tokens * heads * splits * D + row * splits * 2;
-  const float m0 = ml[2 * min(tid, splits - 1)], l0 = ml[2 * min(tid, splits - 1) + 1];
-  const int tiles = (cache_len(c, seqs[i]) + kTileKeys - 1) / kTileKeys;
-  const int n = min((tiles + chunk - 1) / chunk, splits);         // parts that hold anything
-  float mm = tid < n ? m0 : -INFINITY;                            // a thread per part
-#pragma unroll
-  for (int y = 1; y < 64; y <<= 1) mm = fmaxf(mm, __shfl_xor(mm, y));
-  if (lane == 0) red[0][wave] = mm;
-  __syncthreads();
-  mm = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-  const float mu = mm == -INFINITY ? 0.f : mm, f = tid < n ? __builtin_amdgcn_exp2f(m0 - mu) : 0.f;
-  float ll = tid < n ? f * l0 : 0.f;
-  if (tid < kMaxSplits) weight[tid] = f;
-#pragma unroll
-  for (int y = 1; y < 64; y <<= 1) ll += __shfl_xor(ll, y);
-  if (lane == 0) red[1][wave] = ll;
-  __syncthreads();
-  ll = red[1][0] + red[1][1] + red[1][2] + red[1][3];
-  floatx4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = w; s0 < n; s0 += 8 * W) {
-    if (s0 != w) load(s0);
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (s0 + u * W < n) v += weight[s0 + u * W] * x[u];
-  }
-  if (w < W) sum[w][d4] = v;
-  __syncthreads();
-  if (w == 0) {
-#pragma unroll
-    for (int y = 1; y < W; ++y) v += sum[y][d4];
-    struct alignas(4 * sizeof(T)) { T v[4]; } r;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r.v[e] = (T)(ll == 0.f ? 0.f : v[e] / ll);
-    *(decltype(r) *)((T *)out.data + i * out.token_stride + h * out.head_stride + 4 * d4) = r;
-  }
-  if (lse && tid == 0) lse[h * out.tokens + i] = (mm + __builtin_log2f(ll)) * kLn2;
+  const int64_t i = blockIdx.x / heads, h = blockIdx.x % heads;
+  join_parts<T>(blockIdx.x, out.tokens * heads, 32 * G, splits, part,
+                [&] {
+                  const int tiles = (cache_len(c, seqs[i]) + kTileKeys - 1) / kTileKeys;
+                  return min((tiles + chunk - 1) / chunk, splits);
+                },
+                (T *)out.data + i * out.token_stride + h * out.head_stride, lse ? lse + h * out.tokens + i : nullptr);
 }
 
 int64_t keys_of(const ios_attn_desc &d) { return d.max_keys ? d.max_keys : 1 << 16; }

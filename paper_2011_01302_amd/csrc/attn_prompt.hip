@@ -10,7 +10,7 @@
 // half h; V is read in that order).
 #include <type_traits>
 
-#include "decoder.h"
+#include "attn_prompt.h"
 
 namespace ios {
 
@@ -25,10 +25,13 @@ typedef __bf16 bfx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
-constexpr int kBM = 128, kBN = 64;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// the maximum is only followed when it grows by more than 2^8 (p stays below 2^8, the sums are in 32 bits)
-constexpr float kSlack = 8.f;
+constexpr int kBN = 64;
+// Fewer than kFewBlocks workgroups: the keys of a row are spread over workgroups (a second launch joins them), in parts
+// of at least kPartKeys keys.  Up to kTwoGroups: over two groups of waves of one workgroup.
+constexpr int kFewBlocks = 129, kPartKeys = 256, kTwoGroups = 320;
+// p = 2^(score - m), m kTop below the row's largest score when it was last followed, which it is when a score passes it
+// by kTop + 2 (sums are in 32 bits).  f16 then holds p from 2^15 down to 2^-38 of the largest.
+template <class T> constexpr float kTop = std::is_same_v<T, _Float16> ? 13.f : 0.f;
 constexpr uint32_t kOutside = 0x80000000u;       // byte offset past every buffer: reads as 0
 
 template <class T>
@@ -60,13 +63,6 @@ __device__ __forceinline__ void lds_copy16(__amdgpu_buffer_rsrc_t r, unsigned ch
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)l, 16, (int)off, 0, 0, 0);
 }
 
-struct PromptArgs {
-  int heads, ratio, dim, seqs, causal;
-  float scale;
-  ios_tokens q, k, v, out;
-  float *lse;
-  const int32_t *cu_q, *cu_k;
-};
 
 // The two halves of a wave hold different keys of the same queries: this
 // lane's value and the other half's.  (The swap exchanges two registers; given
@@ -78,11 +74,16 @@ __device__ __forceinline__ float other_half(float v) {
   return __builtin_bit_cast(float, threadIdx.x & 32 ? r[0] : r[1]);
 }
 
-template <class T, int DP>
-__global__ __launch_bounds__(256, 2) void attn_prompt_kernel(PromptArgs a) {
+// KG groups of four waves take the tiles in turn and are joined at the end.
+template <class T, int DP, int KG>
+__global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) {
   constexpr int CH = DP / 8, KS = DP / 16, DB = DP / 32, LOADS = kBN * CH / 256;
-  __shared__ __align__(16) unsigned char lds[2][2][kBN * DP * 2];      // [buffer][K, V]
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // the only array in LDS: with a second one the compiler tells them apart, and waits for every copy in flight before
+  // it reads from either
+  __shared__ __align__(16) unsigned char stage[KG][2][2][kBN * DP * 2];   // [group][buffer][K, V]
+  const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  auto &lds = stage[group];
   const int half = lane >> 5, l31 = lane & 31, l15 = lane & 15;
 
   // 128-query tiles: sequence i has tiles from cu_q[i] / 128 + i on; the last tiles, which see most keys, go first
@@ -102,7 +103,12 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(PromptArgs a) {
   auto last_key = [&](int row) { return a.causal ? (int)min((int64_t)min(row, lq - 1) + diff, (int64_t)lk - 1) : lk - 1; };
   const int lim = max(last_key(r0 + l31), -1);
   const int lim_lo = last_key(r0), lim_hi = last_key(r0 + 31);
-  const int tiles = max(last_key(q0 + kBM - 1) + kBN, 0) / kBN;
+  int tiles = max(last_key(q0 + kBM - 1) + kBN, 0) / kBN;
+  const int split = blockIdx.z, t0 = split * a.chunk;
+  if (a.part) {
+    if (split > 0 && t0 >= tiles) return;
+    if (split + 1 < (int)gridDim.z) tiles = min(tiles, t0 + a.chunk);
+  }
 
   // queries, the sign of the scale folded in
   shortx8 qf[KS];
@@ -132,135 +138,288 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(PromptArgs a) {
   }
   const T *kbase = (const T *)a.k.data + ka * a.k.token_stride + kvh * a.k.head_stride;
   const T *vbase = (const T *)a.v.data + ka * a.v.token_stride + kvh * a.v.head_stride;
-  auto issue = [&](int t, int buf) {
-    const __amdgpu_buffer_rsrc_t kr = buffer(kbase + (int64_t)t * kBN * a.k.token_stride);
-    const __amdgpu_buffer_rsrc_t vr = buffer(vbase + (int64_t)t * kBN * a.v.token_stride);
+  auto issue = [&](const T *base, int64_t stride, const uint32_t *off, int t, unsigned char *to) {
+    const __amdgpu_buffer_rsrc_t r = buffer(base + (int64_t)t * kBN * stride);
     const int left = lk - t * kBN;                           // rows past the sequence's last key read as 0
 #pragma unroll
-    for (int p = 0; p < LOADS; ++p) {
-      unsigned char *dk = &lds[buf][0][(p * 256 + wave * 64) * 16], *dv = &lds[buf][1][(p * 256 + wave * 64) * 16];
-      lds_copy16(kr, dk, row_of[p] < left ? koff[p] : kOutside);
-      lds_copy16(vr, dv, row_of[p] < left ? voff[p] : kOutside);
-    }
+    for (int p = 0; p < LOADS; ++p)
+      lds_copy16(r, to + (p * 256 + wave * 64) * 16, row_of[p] < left ? off[p] : kOutside);
   };
+  auto issue_k = [&](int t, int buf) { issue(kbase, a.k.token_stride, koff, t, lds[buf][0]); };
+  auto issue_v = [&](int t, int buf) { issue(vbase, a.v.token_stride, voff, t, lds[buf][1]); };
 
   float m, l;
   floatx16 o[DB];
   const floatx16 zero = {};
 
-  // One walk over the keys.  careful: infinities and NaN among the values of a tile that not every row sees whole
-  // are kept out of the product (0 times one of them is a NaN) and reach the rows that see them by counts.
-  auto walk = [&](auto careful) {
+  // scores of a tile, transposed: keys 32 b + (r & 3) + 8 (r >> 2) + 4 half of query l31
+  auto scores = [&](const unsigned char *sk, floatx16 *s) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      s[b] = zero;
+      const int r = 32 * b + l31;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const shortx8 kf = *(const shortx8 *)(sk + r * (CH * 16) + ((2 * i + half) ^ swz_k<DP>(r)) * 16);
+        s[b] = mfma<T>(kf, qf[i], s[b]);
+      }
+    }
+  };
+  auto hide = [&](int t, floatx16 *s) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (t * kBN + 32 * b + (r & 3) + 8 * (r >> 2) + 4 * half > lim) s[b][r] = -INFINITY;
+  };
+  auto largest = [&](const floatx16 *s) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+    return mx;
+  };
+  // follow the rows' maxima where they have grown, each row by its own scores alone, so that no row's result depends on
+  // another's
+  auto follow = [&](float mx) {
+    mx *= mul;
+    if (__any(mx > m + (kTop<T> + 2.f))) {
+      const float rm = fmaxf(mx, other_half(mx)), mn = rm > m + (kTop<T> + 2.f) ? rm - kTop<T> : m;
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i] *= f;
+    }
+  };
+  auto weights = [&](const floatx16 *s, shortx8 *pf) {
+    const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[b][r], mul, -mu));
+        l += e;
+        pf[2 * b + (r >> 3)][r & 7] = __builtin_bit_cast(short, (T)e);        // p as the inputs' type: 2^-9 (2^-12) each
+      }
+  };
+  auto values = [&](const unsigned char *sv, int i, int ks) {
+    const int r = 16 * ks + 4 * half + (l15 >> 2), c = 4 * i + 2 * (lane >> 4 & 1) + ((l15 & 3) >> 1);
+    const unsigned char *p = sv + r * (CH * 16) + (c ^ swz_v<DP>(r)) * 16 + 8 * (l15 & 1);
+    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)p);
+    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p + 8 * CH * 16));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto clear = [&] {
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
     for (int i = 0; i < DB; ++i) o[i] = zero;
-    if (tiles > 0) issue(0, 0);
-    for (int t = 0; t < tiles; ++t) {
-      // this wave's loads have landed, and every wave is done with the other buffer
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (t + 1 < tiles) issue(t + 1, (t + 1) & 1);
-      if (t * kBN > lim_hi) continue;                        // no row of this wave sees the tile
-      const unsigned char *sk = lds[t & 1][0], *sv = lds[t & 1][1];
-      const bool masked = t * kBN + kBN - 1 > lim_lo;
-      floatx16 s[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        s[b] = zero;
-        const int r = 32 * b + l31;
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          const shortx8 kf = *(const shortx8 *)(sk + r * (CH * 16) + ((2 * i + half) ^ swz_k<DP>(r)) * 16);
-          s[b] = mfma<T>(kf, qf[i], s[b]);
-        }
-      }
-      if (masked) {
-        asm volatile("");                                    // a branch: selects in every tile took a quarter of the walk
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (t * kBN + 32 * b + (r & 3) + 8 * (r >> 2) + 4 * half > lim) s[b][r] = -INFINITY;
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
-      mx *= mul;
-      if (__any(mx > m + kSlack)) {
-        // each row by its own scores alone, so that no row's result depends on another's
-        const float rm = fmaxf(mx, other_half(mx)), mn = rm > m + kSlack ? rm : m;
-        const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= f;
-#pragma unroll
-        for (int i = 0; i < DB; ++i) o[i] *= f;
-      }
-      const float mu = m == -INFINITY ? 0.f : m;
-      shortx8 pf[4];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(s[b][r], mul, -mu));
-          l += e;
-          pf[2 * b + (r >> 3)][r & 7] = __builtin_bit_cast(short, (T)e);      // p as the inputs' type: 2^-9 (2^-12) each
-        }
-#pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        floatx16 nan = zero, up = zero, down = zero;
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          const int r = 16 * ks + 4 * half + (l15 >> 2), c = 4 * i + 2 * (lane >> 4 & 1) + ((l15 & 3) >> 1);
-          const unsigned char *p = sv + r * (CH * 16) + (c ^ swz_v<DP>(r)) * 16 + 8 * (l15 & 1);
-          const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)p);
-          const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p + 8 * CH * 16));
-          shortx8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-          if constexpr (careful) {
-            if (masked) {
-              constexpr int inf = std::is_same_v<T, _Float16> ? 0x7C00 : 0x7F80;
-              const short one = __builtin_bit_cast(short, (T)1.f);
-              shortx8 vn, vu, vd, seen;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int mag = vf[e] & 0x7FFF;
-                vn[e] = mag > inf ? one : 0;
-                vu[e] = vf[e] == inf ? one : 0;
-                vd[e] = mag == inf && vf[e] < 0 ? one : 0;
-                if (mag >= inf) vf[e] = 0;
-                seen[e] = t * kBN + 16 * ks + 4 * half + (e & 3) + 8 * (e >> 2) <= lim ? one : 0;
-              }
-              nan = mfma<T>(vn, seen, nan);
-              up = mfma<T>(vu, seen, up);
-              down = mfma<T>(vd, seen, down);
-            }
-          }
-          o[i] = mfma<T>(vf, pf[ks], o[i]);
-        }
-        if constexpr (careful) {
-          if (masked) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              o[i][r] += nan[r] > 0.f || (up[r] > 0.f && down[r] > 0.f) ? NAN
-                         : up[r] > 0.f ? INFINITY : down[r] > 0.f ? -INFINITY : 0.f;
-          }
-        }
-      }
-    }
   };
+  // this wave's loads have landed, and every wave is done with what they replace
+  auto arrived = [] {
+    __builtin_amdgcn_s_waitcnt(0x0070);                      // vmcnt = lgkmcnt = 0
+    asm volatile("s_barrier" ::: "memory");
+  };
+  auto masked = [&](int t) { return t * kBN + kBN - 1 > lim_lo; };
 
-  walk(std::false_type{});
+  // The walk over the keys.  A wave issues a product every 32 cycles at most, and the vector units are free between:
+  // the next tile's scores are computed while this tile's become weights, this tile's output while the next one's
+  // maxima are looked for.  The compiler keeps that order (it would do one after the other).
+  typedef const __attribute__((address_space(3))) shortx8 lds_shortx8;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)&lds[0][0][0];
+  const uint32_t klane = lds0 + l31 * (CH * 16) + (half ^ swz_k<DP>(l31)) * 16;
+  const int vrow = 4 * half + (l15 >> 2), vchunk = 2 * (lane >> 4 & 1) + ((l15 & 3) >> 1);
+  const uint32_t vlane = lds0 + kBN * DP * 2 + vrow * (CH * 16) + (vchunk ^ swz_v<DP>(vrow)) * 16 + 8 * (l15 & 1);
+  constexpr uint32_t kBuffer = 2 * kBN * DP * 2;
+  // operand c of K Q^T: values 16 (c / 2) .. + 15 of keys 32 (c % 2) .. + 31
+  auto k_operand = [&](uint32_t base, int c) {
+    constexpr int flip = DP == 128 ? 7 : DP == 64 ? 3 : 1;      // the chunk bits that the swizzle covers
+    const int i = c >> 1;
+    return *(lds_shortx8 *)(uintptr_t)((base ^ ((i & flip) << 5)) + ((i & ~flip) << 5) + (c & 1) * 32 * CH * 16);
+  };
+  // operand c of V^T P^T: values 32 (c % DB) .. + 31 of keys 16 (c / DB) .. + 15
+  auto v_operand = [&](uint32_t base, int c) {
+    const int i = c % DB, ks = c / DB;
+    const uint32_t p = (DP == 96 ? base + (i << 6) : base ^ (i << 6)) + ks * 16 * CH * 16;
+    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(uintptr_t)p);
+    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(uintptr_t)(p + 8 * CH * 16));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  clear();
+  {
+    const int first = t0 + group;
+    // past the last tile that a row of this wave sees there is nothing to do but to load and to wait
+    const int end = min(tiles, (lim_hi + kBN) / kBN);
+    // tile k of this group, whose scores are s; leaves those of the next in sn
+    auto step = [&](int k, floatx16 *s, floatx16 *sn) {
+      const int t = first + k * KG, next = t + KG;
+      arrived();
+      if (next < tiles) issue_v(next, (k + 1) & 1);
+      if (next + KG < tiles) issue_k(next + KG, k & 1);
+      if (t >= end) return;
+      const uint32_t kb = klane + ((k + 1) & 1) * kBuffer, vb = vlane + (k & 1) * kBuffer;
+      constexpr int NK = 2 * KS, NV = 4 * DB, AHEAD = 3;
+      shortx8 f[AHEAD + 1], pf[4];
+      const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int c = 0; c < AHEAD; ++c) f[c] = k_operand(kb, c);
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {                         // scores of no tile, and not used, after the last one
+        if (c + AHEAD < NK) f[(c + AHEAD) % (AHEAD + 1)] = k_operand(kb, c + AHEAD);
+        else f[(c + AHEAD) % (AHEAD + 1)] = v_operand(vb, c + AHEAD - NK);
+        sn[c & 1] = mfma<T>(f[c % (AHEAD + 1)], qf[c >> 1], c < 2 ? zero : sn[c & 1]);
+#pragma unroll
+        for (int x = c * 32 / NK; x < (c + 1) * 32 / NK; ++x) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[x >> 4][x & 15], mul, -mu));
+          l += e;
+          pf[x >> 3][x & 7] = __builtin_bit_cast(short, (T)e);                // p as the inputs' type: 2^-9 (2^-12) each
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < NV; ++c) {
+        if (c + AHEAD < NV) f[(c + NK + AHEAD) % (AHEAD + 1)] = v_operand(vb, c + AHEAD);
+        o[c % DB] = mfma<T>(f[(c + NK) % (AHEAD + 1)], pf[c / DB], o[c % DB]);
+#pragma unroll
+        for (int x = c * 32 / NV; x < (c + 1) * 32 / NV; ++x) mx = fmaxf(mx, sn[x & 1][x >> 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (next < end) {
+        if (masked(next)) {
+          hide(next, sn);
+          mx = largest(sn);
+        }
+        follow(mx);
+      }
+    };
+    floatx16 s[2], sn[2];
+    if (first < tiles) issue_k(first, 0);
+    arrived();
+    if (first < tiles) issue_v(first, 0);
+    if (first + KG < tiles) issue_k(first + KG, 1);
+    if (first < end) {
+      scores(lds[0][0], s);
+      if (masked(first)) hide(first, s);
+      follow(largest(s));
+    }
+    for (int k = 0; t0 + k * KG < tiles; k += 2) {
+      step(k, s, sn);
+      if (t0 + (k + 1) * KG < tiles) step(k + 1, sn, s);
+    }
+  }
   int odd = 0;
 #pragma unroll
   for (int i = 0; i < DB; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) odd |= !(__builtin_fabsf(o[i][r]) < INFINITY);
-  if (__syncthreads_or(odd)) walk(std::true_type{});
+  // whether any wave of the workgroup found one
+  int *found = (int *)stage;
+  __syncthreads();                                           // the tiles are done with
+  odd = __any(odd);
+  if (lane == 0) found[threadIdx.x >> 6] = odd;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4 * KG; ++w) odd |= found[w];
+  if (__builtin_amdgcn_readfirstlane(odd)) {
+    // Again, with care: infinities and NaN among the values of a tile that not every row sees whole are kept out of the
+    // product (0 times one of them is a NaN) and reach the rows that see them by counts.
+    clear();
+    for (int k = 0; t0 + k * KG < tiles; ++k) {
+      const int t = t0 + k * KG + group;
+      __syncthreads();
+      if (t < tiles) {
+        issue_k(t, 0);
+        issue_v(t, 0);
+      }
+      arrived();
+      if (t >= tiles || t * kBN > lim_hi) continue;
+      floatx16 s[2];
+      shortx8 pf[4];
+      scores(lds[0][0], s);
+      hide(t, s);
+      follow(largest(s));
+      weights(s, pf);
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        floatx16 nan = zero, up = zero, down = zero;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          shortx8 vf = values(lds[0][1], i, ks);
+          if (masked(t)) {
+            constexpr int inf = std::is_same_v<T, _Float16> ? 0x7C00 : 0x7F80;
+            const short one = __builtin_bit_cast(short, (T)1.f);
+            shortx8 vn, vu, vd, seen;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int mag = vf[e] & 0x7FFF;
+              vn[e] = mag > inf ? one : 0;
+              vu[e] = vf[e] == inf ? one : 0;
+              vd[e] = mag == inf && vf[e] < 0 ? one : 0;
+              if (mag >= inf) vf[e] = 0;
+              seen[e] = t * kBN + 16 * ks + 4 * half + (e & 3) + 8 * (e >> 2) <= lim ? one : 0;
+            }
+            nan = mfma<T>(vn, seen, nan);
+            up = mfma<T>(vu, seen, up);
+            down = mfma<T>(vd, seen, down);
+          }
+          o[i] = mfma<T>(vf, pf[ks], o[i]);
+        }
+        if (masked(t)) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            o[i][r] += nan[r] > 0.f || (up[r] > 0.f && down[r] > 0.f) ? NAN
+                       : up[r] > 0.f ? INFINITY : down[r] > 0.f ? -INFINITY : 0.f;
+        }
+      }
+    }
+  }
 
   l += other_half(l);
+  if constexpr (KG > 1) {                                    // the second group's rows go through LDS to the first
+    static_assert(KG == 2 && sizeof(stage) >= (4 * DB * 16 * 64 + 512) * 4, "one other group");
+    __syncthreads();                                         // the tiles are done with
+    float *oo = (float *)stage + wave * (DB * 16 * 64) + lane, *ml = (float *)stage + 4 * DB * 16 * 64 + tid;
+    if (group == 1) {
+      ml[0] = m;
+      ml[256] = l;
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oo[(i * 16 + r) * 64] = o[i][r];
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float m1 = ml[0], mm = fmaxf(m, m1), mu = mm == -INFINITY ? 0.f : mm;
+    const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(m1 - mu);
+    m = mm;
+    l = l * f0 + ml[256] * f1;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * f0 + oo[(i * 16 + r) * 64] * f1;
+  }
   const int row = r0 + l31;
   if (row >= lq) return;
+  if (a.part) {
+    const int64_t x = (qa + row) * a.heads + head;
+    float *dst = a.part + (x * gridDim.z + split) * a.dim;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        if (32 * i + 8 * r4 + 4 * half < a.dim)
+          *(floatx4 *)(dst + 32 * i + 8 * r4 + 4 * half) =
+              floatx4{o[i][4 * r4], o[i][4 * r4 + 1], o[i][4 * r4 + 2], o[i][4 * r4 + 3]};
+    if (half == 0) {
+      float *ml = a.part + (int64_t)a.q.tokens * a.heads * gridDim.z * a.dim + (x * gridDim.z + split) * 2;
+      ml[0] = m;
+      ml[1] = l;
+    }
+    return;
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T *dst = (T *)a.out.data + (qa + row) * a.out.token_stride + head * a.out.head_stride;
 #pragma unroll
@@ -278,33 +437,73 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_kernel(PromptArgs a) {
   if (a.lse && half == 0) a.lse[(int64_t)head * a.q.tokens + qa + row] = (m + __builtin_log2f(l)) * kLn2;
 }
 
-template <class T, int DP>
-hipError_t run(const PromptArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((attn_prompt_kernel<T, DP>), dim3((unsigned)(a.q.tokens / kBM + a.seqs), a.heads), dim3(256), 0, s, a);
+// The rows' parts: a workgroup per row.  Rows of no sequence are passed over.
+template <class T>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int splits, int tile_keys) {
+  const int64_t i = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
+  if (i < clip(a.cu_q[0], a.q.tokens) || i >= clip(a.cu_q[a.seqs], a.q.tokens)) return;
+  join_parts<T>(blockIdx.x, a.q.tokens * a.heads, a.dim, splits, a.part,
+                [&] {
+                  // the workgroup's tiles, as the first launch counted them
+                  const int seq = find_row(a.seqs, i, [&](int s) { return clip(a.cu_q[s], a.q.tokens); });
+                  const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
+                  const int64_t lq = clip(a.cu_q[seq + 1], a.q.tokens) - qa;
+                  const int64_t lk = max(clip(a.cu_k[seq + 1], a.k.tokens) - ka, (int64_t)0);
+                  const int64_t row = (i - qa) / kBM * kBM + kBM - 1;
+                  const int64_t last = a.causal ? min(min(row, lq - 1) + lk - lq, lk - 1) : lk - 1;
+                  const int64_t tiles = max(last + tile_keys, (int64_t)0) / tile_keys;
+                  return (int)min(max((tiles + a.chunk - 1) / a.chunk, (int64_t)1), (int64_t)splits);
+                },
+                (T *)a.out.data + i * a.out.token_stride + h * a.out.head_stride,
+                a.lse ? a.lse + h * a.q.tokens + i : nullptr);
+}
+
+template <class T>
+hipError_t join(const PromptArgs &a, int splits, int tile_keys, hipStream_t s) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  hipLaunchKernelGGL((prompt_join_kernel<T>), dim3((unsigned)(a.q.tokens * a.heads)), dim3(256), 0, s, a, splits, tile_keys);
   return hipGetLastError();
 }
+
+int64_t prompt_blocks(const ios_attn_desc &d, int64_t q_tokens) { return (q_tokens / kBM + d.seqs) * d.heads; }
+
+template <class T, int DP>
+hipError_t run(const PromptArgs &a, bool two, int splits, hipStream_t s) {
+  const dim3 grid((unsigned)(a.q.tokens / kBM + a.seqs), a.heads, splits);
+  if (two) hipLaunchKernelGGL((attn_prompt_kernel<T, DP, 2>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((attn_prompt_kernel<T, DP, 1>), grid, dim3(256), 0, s, a);
+  return join<T>(a, splits, kBN, s);
+}
 template <class T>
-hipError_t for_dim(const PromptArgs &a, hipStream_t s) {
-  if (a.dim <= 32) return run<T, 32>(a, s);
-  if (a.dim <= 64) return run<T, 64>(a, s);
-  if (a.dim <= 96) return run<T, 96>(a, s);
-  return run<T, 128>(a, s);
+hipError_t for_dim(const PromptArgs &a, bool two, int splits, hipStream_t s) {
+  if (a.dim <= 32) return run<T, 32>(a, two, splits, s);
+  if (a.dim <= 64) return run<T, 64>(a, two, splits, s);
+  if (a.dim <= 96) return run<T, 96>(a, two, splits, s);
+  return run<T, 128>(a, two, splits, s);
 }
 
 }  // namespace
 
-hipError_t launch_attn_prompt_float(const ios_attn_desc &d, const ios_tokens &q, const ios_tokens &k,
-                                    const ios_tokens &v, const ios_tokens &out, float *lse, const int32_t *cu_q,
-                                    const int32_t *cu_k, hipStream_t s);
-
-int prompt_splits(const ios_attn_desc &, int64_t) { return 1; }
+int prompt_splits(const ios_attn_desc &d, int64_t q_tokens) {
+  const int64_t blocks = prompt_blocks(d, q_tokens);
+  if (blocks >= kFewBlocks || blocks == 0) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / blocks, d.max_keys / kPartKeys), kMaxParts));
+}
 
 hipError_t launch_attn_prompt(const ios_attn_desc &d, const ios_tokens &q, const ios_tokens &k, const ios_tokens &v,
-                              const ios_tokens &out, float *lse, const int32_t *cu_q, const int32_t *cu_k, void *,
-                              int, hipStream_t s) {
-  if (d.dtype == IOS_F32) return launch_attn_prompt_float(d, q, k, v, out, lse, cu_q, cu_k, s);
-  const PromptArgs a{d.heads, d.heads / d.kv_heads, d.head_dim, d.seqs, d.causal, d.scale, q, k, v, out, lse, cu_q, cu_k};
-  return d.dtype == IOS_F16 ? for_dim<_Float16>(a, s) : for_dim<__bf16>(a, s);
+                              const ios_tokens &out, float *lse, const int32_t *cu_q, const int32_t *cu_k, void *work,
+                              int splits, hipStream_t s) {
+  PromptArgs a{d.heads, d.heads / d.kv_heads, d.head_dim, d.seqs, d.causal, d.scale, q, k, v, out, lse, cu_q, cu_k,
+               splits > 1 ? (float *)work : nullptr, 1 << 24};
+  const int tile_keys = d.dtype == IOS_F32 ? kFloatKeys : kBN;
+  if (splits > 1) a.chunk = std::max(1, (int)(((int64_t)d.max_keys + (int64_t)tile_keys * splits - 1) / ((int64_t)tile_keys * splits)));
+  const bool two = splits == 1 && prompt_blocks(d, q.tokens) <= kTwoGroups;
+  if (d.dtype == IOS_F32) {
+    hipError_t e = launch_attn_prompt_float(a, two, splits, s);
+    return e == hipSuccess ? join<float>(a, splits, tile_keys, s) : e;
+  }
+  return d.dtype == IOS_F16 ? for_dim<_Float16>(a, two, splits, s) : for_dim<__bf16>(a, two, splits, s);
 }
 
 }  // namespace ios

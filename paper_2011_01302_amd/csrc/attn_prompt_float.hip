@@ -2,32 +2,26 @@
 // attn_prompt.hip on v_mfma_f32_32x32x2_f32, every number in 32 bits.  Bound by
 // the fp32 matrix rate, an eighth of the 16-bit one, so plain staging of tiles
 // of 32 keys through registers is enough.
-#include "decoder.h"
+#include "attn_prompt.h"
 
 namespace ios {
 
 namespace {
 
-typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr int kBM = 128, kBN = 32;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kBN = kFloatKeys;
 
-struct PromptArgs {
-  int heads, ratio, dim, seqs, causal;
-  float scale;
-  ios_tokens q, k, v, out;
-  float *lse;
-  const int32_t *cu_q, *cu_k;
-};
 
-template <int DP>
-__global__ __launch_bounds__(256, 2) void attn_prompt_float_kernel(PromptArgs a) {
+template <int DP, int KG>
+__global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptArgs a) {
   constexpr int CH = DP / 4, DB = DP / 32, PITCH = DP + 4, LOADS = kBN * CH / 256;
-  __shared__ __align__(16) float sk[kBN * PITCH], sv[kBN * PITCH];
-  __shared__ int odd_rows[2][kBN];            // of this tile and the next: waves may be a tile apart
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ __align__(16) float stage[KG][2][kBN * PITCH];
+  __shared__ float other_o[KG > 1 ? 256 : 1][17], other_ml[KG > 1 ? 256 : 1][2];
+  __shared__ int odd_rows[KG][2][kBN];            // of this tile and the next: waves may be a tile apart
+  const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  float *sk = stage[group][0], *sv = stage[group][1];
   const int half = lane >> 5, l31 = lane & 31;
 
   const int64_t x = gridDim.x - 1 - blockIdx.x;
@@ -44,7 +38,12 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_float_kernel(PromptArgs a)
   auto last_key = [&](int row) { return a.causal ? (int)min((int64_t)min(row, lq - 1) + diff, (int64_t)lk - 1) : lk - 1; };
   const int lim = max(last_key(r0 + l31), -1);
   const int lim_lo = last_key(r0), lim_hi = last_key(r0 + 31);
-  const int tiles = max(last_key(q0 + kBM - 1) + kBN, 0) / kBN;
+  int tiles = max(last_key(q0 + kBM - 1) + kBN, 0) / kBN;
+  const int split = blockIdx.z, t0 = split * a.chunk;
+  if (a.part) {
+    if (split > 0 && t0 >= tiles) return;
+    if (split + 1 < (int)gridDim.z) tiles = min(tiles, t0 + a.chunk);
+  }
 
   // Q: values 8 i + 4 half + e of query l31 (the order in which K's are read)
   float qf[DP / 2];
@@ -81,9 +80,10 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_float_kernel(PromptArgs a)
       }
     }
   };
-  if (tiles > 0) load(0);
-  for (int t = 0; t < tiles; ++t) {
-    int *odd_row = odd_rows[t & 1];
+  if (t0 + group < tiles) load(t0 + group);
+  for (int k = 0; t0 + k * KG < tiles; ++k) {
+    const int t = t0 + k * KG + group;
+    int *odd_row = odd_rows[group][k & 1];
     if (tid < kBN) odd_row[tid] = 0;
     __syncthreads();
 #pragma unroll
@@ -97,8 +97,8 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_float_kernel(PromptArgs a)
       if (odd) odd_row[r] = 1;
     }
     __syncthreads();
-    if (t + 1 < tiles) load(t + 1);
-    if (t * kBN > lim_hi) continue;
+    if (t + KG < tiles) load(t + KG);
+    if (t >= tiles || t * kBN > lim_hi) continue;
     floatx16 s = zero;
 #pragma unroll
     for (int i = 0; i < DP / 8; ++i) {
@@ -159,8 +159,50 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_float_kernel(PromptArgs a)
   }
 
   l += __shfl_xor(l, 32);
+  if constexpr (KG > 1) {                                    // the second group's rows go through LDS to the first
+    if (group == 1) {
+      other_ml[tid][0] = m;
+      other_ml[tid][1] = l;
+    }
+    __syncthreads();
+    const float m1 = other_ml[tid][0], mm = fmaxf(m, m1), mu = mm == -INFINITY ? 0.f : mm;
+    const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(m1 - mu);
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+      if (group == 1) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) other_o[tid][r] = o[i][r];
+      }
+      __syncthreads();
+      if (group == 0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * f0 + other_o[tid][r] * f1;
+      }
+      __syncthreads();
+    }
+    if (group == 1) return;
+    m = mm;
+    l = l * f0 + other_ml[tid][1] * f1;
+  }
   const int row = r0 + l31;
   if (row >= lq) return;
+  if (a.part) {
+    const int64_t x = (qa + row) * a.heads + head;
+    float *dst = a.part + (x * gridDim.z + split) * a.dim;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        if (32 * i + 8 * r4 + 4 * half < a.dim)
+          *(floatx4 *)(dst + 32 * i + 8 * r4 + 4 * half) =
+              floatx4{o[i][4 * r4], o[i][4 * r4 + 1], o[i][4 * r4 + 2], o[i][4 * r4 + 3]};
+    if (half == 0) {
+      float *ml = a.part + (int64_t)a.q.tokens * a.heads * gridDim.z * a.dim + (x * gridDim.z + split) * 2;
+      ml[0] = m;
+      ml[1] = l;
+    }
+    return;
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   float *dst = (float *)a.out.data + (qa + row) * a.out.token_stride + head * a.out.head_stride;
 #pragma unroll
@@ -179,21 +221,20 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_float_kernel(PromptArgs a)
 }
 
 template <int DP>
-hipError_t run(const PromptArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((attn_prompt_float_kernel<DP>), dim3((unsigned)(a.q.tokens / kBM + a.seqs), a.heads), dim3(256), 0, s, a);
+hipError_t run(const PromptArgs &a, bool two, int splits, hipStream_t s) {
+  const dim3 grid((unsigned)(a.q.tokens / kBM + a.seqs), a.heads, splits);
+  if (two) hipLaunchKernelGGL((attn_prompt_float_kernel<DP, 2>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((attn_prompt_float_kernel<DP, 1>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attn_prompt_float(const ios_attn_desc &d, const ios_tokens &q, const ios_tokens &k,
-                                    const ios_tokens &v, const ios_tokens &out, float *lse, const int32_t *cu_q,
-                                    const int32_t *cu_k, hipStream_t s) {
-  const PromptArgs a{d.heads, d.heads / d.kv_heads, d.head_dim, d.seqs, d.causal, d.scale, q, k, v, out, lse, cu_q, cu_k};
-  if (a.dim <= 32) return run<32>(a, s);
-  if (a.dim <= 64) return run<64>(a, s);
-  if (a.dim <= 96) return run<96>(a, s);
-  return run<128>(a, s);
+hipError_t launch_attn_prompt_float(const PromptArgs &a, bool two, int splits, hipStream_t s) {
+  if (a.dim <= 32) return run<32>(a, two, splits, s);
+  if (a.dim <= 64) return run<64>(a, two, splits, s);
+  if (a.dim <= 96) return run<96>(a, two, splits, s);
+  return run<128>(a, two, splits, s);
 }
 
 }  // namespace ios

@@ -76,6 +76,18 @@ __device__ __forceinline__ int find_owner(int n, int64_t x, F start) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// The same by halves, for a thread by itself.
+template <class F>
+__device__ __forceinline__ int find_row(int n, int64_t x, F start) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start(mid) <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
 __device__ __forceinline__ int64_t clip(int64_t v, int64_t n) { return v < 0 ? 0 : v > n ? n : v; }
 
 // One head's tile that holds token `pos` of a slot; null where the table has

@@ -211,7 +211,7 @@ def test_prompt_growing_scores(typ):
     check_prompt(typ, q, up.flip(0).contiguous(), v, [n], [n], 0, 1.0)
 
 
-@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("typ", ["f16", "bf16", "f32"])
 def test_prompt_few_rows_many_keys(typ):
     """With a workspace the keys of few rows are spread over workgroups; the result agrees with and without."""
     dt = TYPES[typ][0]
@@ -219,6 +219,33 @@ def test_prompt_few_rows_many_keys(typ):
     q, k, v = randn((50, 4, 64), dt, 1), randn((8000, 2, 64), dt, 2), randn((8000, 2, 64), dt, 3)
     check_prompt(typ, q, k, v, lq, lk, 1)
     check_prompt(typ, q, k, v, lq, lk, 1, work=False)
+
+
+@pytest.mark.parametrize("typ", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 200])
+def test_prompt_long_tail(typ, rows):
+    """One key far ahead of 6000 equal ones, whose weights (2^-16.6) sum to 0.06."""
+    dt, n = TYPES[typ][0], 6000
+    q = torch.zeros(rows, 1, 32, dtype=dt, device=DEV)
+    q[:, :, 0] = 1.0
+    k, v = torch.zeros(n, 1, 32, dtype=dt, device=DEV), torch.ones(n, 1, 32, dtype=dt, device=DEV)
+    k[77, 0, 0], v[77] = 11.5, -1.0
+    check_prompt(typ, q, k, v, [rows], [n], 0, 1.0)
+
+
+@pytest.mark.parametrize("typ", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("lead", [11.5, 18.0])
+def test_decode_long_tail(typ, lead):
+    """As above over the cache; with a lead of 18 each of the others weighs 2^-26."""
+    n = 50000 if lead > 12 else 6000
+    c = Cache(1, 32, 256, 200, 1, 200)
+    c.place([n])
+    k, v = torch.zeros(n, 1, 32, device=DEV), torch.ones(n, 1, 32, device=DEV)
+    k[77, 0, 0], v[77] = lead, -1.0
+    c.append(k, v, [0], [n], "f32")
+    q = torch.zeros(1, 1, 32, dtype=TYPES[typ][0], device=DEV)
+    q[:, :, 0] = 1.0
+    check_decode(typ, c, q, [0], [held(k)], [held(v)], [n], max_keys=n, scale=1.0)
 
 
 def test_prompt_many_sequences():
