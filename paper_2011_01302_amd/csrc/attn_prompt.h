@@ -18,6 +18,18 @@ struct PromptArgs {
   int chunk;
 };
 
+#if defined(__HIPCC__)
+// The workgroup's head and its tile of kBM queries: sequence i has tiles from cu_q[i] / kBM + i on.  All heads' last
+// tiles, which see most keys, go first (with a whole head after the other, the last head's longest tile began when the
+// others' were done: a third of the time of 8192 causal tokens), and heads that share keys go to one XCD (workgroups
+// go to the eight in turn), whose L2 they share.
+__device__ __forceinline__ int prompt_block(const PromptArgs &a, int64_t *tile) {
+  const unsigned h = blockIdx.x % a.heads;
+  *tile = (gridDim.x - 1 - blockIdx.x) / a.heads;
+  return a.heads % 8 ? h : h % 8 * (a.heads / 8) + h / 8;
+}
+#endif
+
 hipError_t launch_attn_prompt_float(const PromptArgs &a, bool two, int splits, hipStream_t s);
 
 }  // namespace ios

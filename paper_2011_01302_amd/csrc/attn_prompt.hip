@@ -86,8 +86,8 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
   auto &lds = stage[group];
   const int half = lane >> 5, l31 = lane & 31, l15 = lane & 15;
 
-  // 128-query tiles: sequence i has tiles from cu_q[i] / 128 + i on; the last tiles, which see most keys, go first
-  const int64_t x = gridDim.x - 1 - blockIdx.x;
+  int64_t x;
+  const int head = prompt_block(a, &x);
   auto start = [&](int i) { return clip(a.cu_q[i], a.q.tokens) / kBM + i; };
   const int seq = find_owner(a.seqs, x, start);
   const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
   const int64_t tile = x - start(seq);
   if (tile * kBM >= lq) return;
   const int q0 = (int)tile * kBM, r0 = q0 + 32 * wave;
-  const int head = blockIdx.y, kvh = head / a.ratio;
+  const int kvh = head / a.ratio;
 
   // last key that a row sees (-1: none); rows past the sequence see what its last row sees
   const int64_t diff = (int64_t)lk - lq;
@@ -470,7 +470,7 @@ int64_t prompt_blocks(const ios_attn_desc &d, int64_t q_tokens) { return (q_toke
 
 template <class T, int DP>
 hipError_t run(const PromptArgs &a, bool two, int splits, hipStream_t s) {
-  const dim3 grid((unsigned)(a.q.tokens / kBM + a.seqs), a.heads, splits);
+  const dim3 grid((unsigned)((a.q.tokens / kBM + a.seqs) * a.heads), 1, splits);
   if (two) hipLaunchKernelGGL((attn_prompt_kernel<T, DP, 2>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((attn_prompt_kernel<T, DP, 1>), grid, dim3(256), 0, s, a);
   return join<T>(a, splits, kBN, s);

@@ -24,7 +24,8 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptAr
   float *sk = stage[group][0], *sv = stage[group][1];
   const int half = lane >> 5, l31 = lane & 31;
 
-  const int64_t x = gridDim.x - 1 - blockIdx.x;
+  int64_t x;
+  const int head = prompt_block(a, &x);
   auto start = [&](int i) { return clip(a.cu_q[i], a.q.tokens) / kBM + i; };
   const int seq = find_owner(a.seqs, x, start);
   const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
@@ -33,7 +34,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptAr
   const int64_t tile = x - start(seq);
   if (tile * kBM >= lq) return;
   const int q0 = (int)tile * kBM, r0 = q0 + 32 * wave;
-  const int head = blockIdx.y, kvh = head / a.ratio;
+  const int kvh = head / a.ratio;
   const int64_t diff = (int64_t)lk - lq;
   auto last_key = [&](int row) { return a.causal ? (int)min((int64_t)min(row, lq - 1) + diff, (int64_t)lk - 1) : lk - 1; };
   const int lim = max(last_key(r0 + l31), -1);
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptAr
 
 template <int DP>
 hipError_t run(const PromptArgs &a, bool two, int splits, hipStream_t s) {
-  const dim3 grid((unsigned)(a.q.tokens / kBM + a.seqs), a.heads, splits);
+  const dim3 grid((unsigned)((a.q.tokens / kBM + a.seqs) * a.heads), 1, splits);
   if (two) hipLaunchKernelGGL((attn_prompt_float_kernel<DP, 2>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((attn_prompt_float_kernel<DP, 1>), grid, dim3(256), 0, s, a);
   return hipGetLastError();

@@ -35,8 +35,8 @@ int type_size(int dtype) { return dtype == IOS_F32 ? 4 : 2; }
 
 // Tokens of a call are bounded so that offsets and grids stay in 32 bits (the
 // elements' own offsets are 64-bit everywhere).
-constexpr int64_t kMaxTokens = (int64_t)1 << 30;
-constexpr int32_t kMaxSeqs = 1 << 22, kMaxAttnSeqs = 65535;
+constexpr int64_t kMaxTokens = (int64_t)1 << 28;
+constexpr int32_t kMaxSeqs = 1 << 21, kMaxAttnSeqs = 65535;
 constexpr int32_t kMaxHeads = 1 << 14;
 // a tile of 64 rows is addressed with 32-bit byte offsets from its first
 constexpr int64_t kMaxStride = (int64_t)1 << 22;
@@ -179,6 +179,7 @@ extern "C" int ios_attn_prompt(const ios_attn_desc *d, const ios_tokens *q, cons
     need(q->tokens == out->tokens, IOS_E_SHAPE, "q and out have different lengths");
     need(cu_q && cu_k, IOS_E_ARG, "null offsets");
     if (q->tokens == 0) return;
+    need((q->tokens / 128 + d->seqs) * d->heads < ((int64_t)1 << 32) / 512, IOS_E_UNSUPPORTED, "too many queries and heads");
     const int splits = usable(prompt_splits(*d, q->tokens), q->tokens, *d, work, work_bytes);
     launched(launch_attn_prompt(*d, *q, *k, *v, *out, lse, cu_q, cu_k, work, splits, (hipStream_t)hip_stream),
              "ios_attn_prompt");
