@@ -5,8 +5,8 @@
 
 namespace ios {
 
-constexpr int kBM = 128;                 // queries of a workgroup
-constexpr int kFloatKeys = 32;           // keys of a float32 tile
+// queries of a workgroup and keys of its tiles
+constexpr int kRows = 128, kKeys = 64, kFloatRows = 64, kFloatKeys = 32;
 
 struct PromptArgs {
   int heads, ratio, dim, seqs, causal;
@@ -16,10 +16,11 @@ struct PromptArgs {
   const int32_t *cu_q, *cu_k;
   float *part;                   // parts of the rows' keys, chunk tiles each (null: whole rows)
   int chunk;
+  int rows, keys;                // of a workgroup and of a tile
 };
 
 #if defined(__HIPCC__)
-// The workgroup's head and its tile of kBM queries: sequence i has tiles from cu_q[i] / kBM + i on.  All heads' last
+// The workgroup's head and its tile of a.rows queries: sequence i has tiles from cu_q[i] / rows + i on.  All heads' last
 // tiles, which see most keys, go first (with a whole head after the other, the last head's longest tile began when the
 // others' were done: a third of the time of 8192 causal tokens), and heads that share keys go to one XCD (workgroups
 // go to the eight in turn), whose L2 they share.
@@ -30,6 +31,6 @@ __device__ __forceinline__ int prompt_block(const PromptArgs &a, int64_t *tile) 
 }
 #endif
 
-hipError_t launch_attn_prompt_float(const PromptArgs &a, bool two, int splits, hipStream_t s);
+hipError_t launch_attn_prompt_float(const PromptArgs &a, int splits, hipStream_t s);
 
 }  // namespace ios

@@ -25,7 +25,7 @@ typedef __bf16 bfx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
-constexpr int kBN = 64;
+constexpr int kBM = kRows, kBN = kKeys;
 // Fewer than kFewBlocks workgroups: the keys of a row are spread over workgroups (a second launch joins them), in parts
 // of at least kPartKeys keys.  Up to kTwoGroups: over two groups of waves of one workgroup.
 constexpr int kFewBlocks = 129, kPartKeys = 256, kTwoGroups = 320;
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
 
 // The rows' parts: a workgroup per row.  Rows of no sequence are passed over.
 template <class T>
-__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int splits, int tile_keys) {
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int splits) {
   const int64_t i = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
   if (i < clip(a.cu_q[0], a.q.tokens) || i >= clip(a.cu_q[a.seqs], a.q.tokens)) return;
   join_parts<T>(blockIdx.x, a.q.tokens * a.heads, a.dim, splits, a.part,
@@ -449,9 +449,9 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int spli
                   const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
                   const int64_t lq = clip(a.cu_q[seq + 1], a.q.tokens) - qa;
                   const int64_t lk = max(clip(a.cu_k[seq + 1], a.k.tokens) - ka, (int64_t)0);
-                  const int64_t row = (i - qa) / kBM * kBM + kBM - 1;
+                  const int64_t row = (i - qa) / a.rows * a.rows + a.rows - 1;
                   const int64_t last = a.causal ? min(min(row, lq - 1) + lk - lq, lk - 1) : lk - 1;
-                  const int64_t tiles = max(last + tile_keys, (int64_t)0) / tile_keys;
+                  const int64_t tiles = max(last + a.keys, (int64_t)0) / a.keys;
                   return (int)min(max((tiles + a.chunk - 1) / a.chunk, (int64_t)1), (int64_t)splits);
                 },
                 (T *)a.out.data + i * a.out.token_stride + h * a.out.head_stride,
@@ -459,21 +459,23 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int spli
 }
 
 template <class T>
-hipError_t join(const PromptArgs &a, int splits, int tile_keys, hipStream_t s) {
+hipError_t join(const PromptArgs &a, int splits, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
-  hipLaunchKernelGGL((prompt_join_kernel<T>), dim3((unsigned)(a.q.tokens * a.heads)), dim3(256), 0, s, a, splits, tile_keys);
+  hipLaunchKernelGGL((prompt_join_kernel<T>), dim3((unsigned)(a.q.tokens * a.heads)), dim3(256), 0, s, a, splits);
   return hipGetLastError();
 }
 
-int64_t prompt_blocks(const ios_attn_desc &d, int64_t q_tokens) { return (q_tokens / kBM + d.seqs) * d.heads; }
+int64_t prompt_blocks(const ios_attn_desc &d, int64_t q_tokens) {
+  return (q_tokens / (d.dtype == IOS_F32 ? kFloatRows : kRows) + d.seqs) * d.heads;
+}
 
 template <class T, int DP>
 hipError_t run(const PromptArgs &a, bool two, int splits, hipStream_t s) {
   const dim3 grid((unsigned)((a.q.tokens / kBM + a.seqs) * a.heads), 1, splits);
   if (two) hipLaunchKernelGGL((attn_prompt_kernel<T, DP, 2>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((attn_prompt_kernel<T, DP, 1>), grid, dim3(256), 0, s, a);
-  return join<T>(a, splits, kBN, s);
+  return join<T>(a, splits, s);
 }
 template <class T>
 hipError_t for_dim(const PromptArgs &a, bool two, int splits, hipStream_t s) {
@@ -494,15 +496,15 @@ int prompt_splits(const ios_attn_desc &d, int64_t q_tokens) {
 hipError_t launch_attn_prompt(const ios_attn_desc &d, const ios_tokens &q, const ios_tokens &k, const ios_tokens &v,
                               const ios_tokens &out, float *lse, const int32_t *cu_q, const int32_t *cu_k, void *work,
                               int splits, hipStream_t s) {
+  const bool f32 = d.dtype == IOS_F32;
   PromptArgs a{d.heads, d.heads / d.kv_heads, d.head_dim, d.seqs, d.causal, d.scale, q, k, v, out, lse, cu_q, cu_k,
-               splits > 1 ? (float *)work : nullptr, 1 << 24};
-  const int tile_keys = d.dtype == IOS_F32 ? kFloatKeys : kBN;
-  if (splits > 1) a.chunk = std::max(1, (int)(((int64_t)d.max_keys + (int64_t)tile_keys * splits - 1) / ((int64_t)tile_keys * splits)));
-  const bool two = splits == 1 && prompt_blocks(d, q.tokens) <= kTwoGroups;
-  if (d.dtype == IOS_F32) {
-    hipError_t e = launch_attn_prompt_float(a, two, splits, s);
-    return e == hipSuccess ? join<float>(a, splits, tile_keys, s) : e;
+               splits > 1 ? (float *)work : nullptr, 1 << 24, f32 ? kFloatRows : kRows, f32 ? kFloatKeys : kKeys};
+  if (splits > 1) a.chunk = std::max(1, (int)(((int64_t)d.max_keys + (int64_t)a.keys * splits - 1) / ((int64_t)a.keys * splits)));
+  if (f32) {
+    const hipError_t e = launch_attn_prompt_float(a, splits, s);
+    return e == hipSuccess ? join<float>(a, splits, s) : e;
   }
+  const bool two = splits == 1 && prompt_blocks(d, q.tokens) <= kTwoGroups;
   return d.dtype == IOS_F16 ? for_dim<_Float16>(a, two, splits, s) : for_dim<__bf16>(a, two, splits, s);
 }
 

@@ -10,17 +10,19 @@ namespace {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr int kBN = kFloatKeys;
+constexpr int kBM = kFloatRows, kBN = kFloatKeys, kRW = kBM / 32, kGroupThreads = 64 * kRW, KG = 2;
 
 
-template <int DP, int KG>
-__global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptArgs a) {
-  constexpr int CH = DP / 4, DB = DP / 32, PITCH = DP + 4, LOADS = kBN * CH / 256;
+// Two waves of 32 queries, and two groups of such waves that take the tiles in turn and are joined at the end: the
+// matrix cores are what bounds, so the work is cut small enough to come out even over them.
+template <int DP>
+__global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kernel(PromptArgs a) {
+  constexpr int CH = DP / 4, DB = DP / 32, PITCH = DP + 4, LOADS = kBN * CH / kGroupThreads;
   __shared__ __align__(16) float stage[KG][2][kBN * PITCH];
-  __shared__ float other_o[KG > 1 ? 256 : 1][17], other_ml[KG > 1 ? 256 : 1][2];
+  __shared__ float other_o[kGroupThreads][17], other_ml[kGroupThreads][2];
   __shared__ int odd_rows[KG][2][kBN];            // of this tile and the next: waves may be a tile apart
-  const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  const int tid = threadIdx.x % kGroupThreads, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / kGroupThreads);
   float *sk = stage[group][0], *sv = stage[group][1];
   const int half = lane >> 5, l31 = lane & 31;
 
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptAr
   auto load = [&](int t) {
 #pragma unroll
     for (int p = 0; p < LOADS; ++p) {
-      const int s = p * 256 + tid, r = s / CH, d = s % CH * 4;
+      const int s = p * kGroupThreads + tid, r = s / CH, d = s % CH * 4;
       nk[p] = nv[p] = floatx4{0.f, 0.f, 0.f, 0.f};
       if (t * kBN + r < lk && d < a.dim) {
         nk[p] = *(const floatx4 *)(kbase + (int64_t)(t * kBN + r) * a.k.token_stride + d);
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptAr
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < LOADS; ++p) {
-      const int s = p * 256 + tid, r = s / CH, d = s % CH * 4;
+      const int s = p * kGroupThreads + tid, r = s / CH, d = s % CH * 4;
       *(floatx4 *)(sk + r * PITCH + d) = nk[p];
       *(floatx4 *)(sv + r * PITCH + d) = nv[p];
       bool odd = false;
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptAr
   }
 
   l += __shfl_xor(l, 32);
-  if constexpr (KG > 1) {                                    // the second group's rows go through LDS to the first
+  {                                                          // the second group's rows go through LDS to the first
     if (group == 1) {
       other_ml[tid][0] = m;
       other_ml[tid][1] = l;
@@ -222,20 +224,19 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_float_kernel(PromptAr
 }
 
 template <int DP>
-hipError_t run(const PromptArgs &a, bool two, int splits, hipStream_t s) {
+hipError_t run(const PromptArgs &a, int splits, hipStream_t s) {
   const dim3 grid((unsigned)((a.q.tokens / kBM + a.seqs) * a.heads), 1, splits);
-  if (two) hipLaunchKernelGGL((attn_prompt_float_kernel<DP, 2>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((attn_prompt_float_kernel<DP, 1>), grid, dim3(256), 0, s, a);
+  hipLaunchKernelGGL((attn_prompt_float_kernel<DP>), grid, dim3(kGroupThreads * KG), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attn_prompt_float(const PromptArgs &a, bool two, int splits, hipStream_t s) {
-  if (a.dim <= 32) return run<32>(a, two, splits, s);
-  if (a.dim <= 64) return run<64>(a, two, splits, s);
-  if (a.dim <= 96) return run<96>(a, two, splits, s);
-  return run<128>(a, two, splits, s);
+hipError_t launch_attn_prompt_float(const PromptArgs &a, int splits, hipStream_t s) {
+  if (a.dim <= 32) return run<32>(a, splits, s);
+  if (a.dim <= 64) return run<64>(a, splits, s);
+  if (a.dim <= 96) return run<96>(a, splits, s);
+  return run<128>(a, splits, s);
 }
 
 }  // namespace ios

@@ -179,7 +179,7 @@ extern "C" int ios_attn_prompt(const ios_attn_desc *d, const ios_tokens *q, cons
     need(q->tokens == out->tokens, IOS_E_SHAPE, "q and out have different lengths");
     need(cu_q && cu_k, IOS_E_ARG, "null offsets");
     if (q->tokens == 0) return;
-    need((q->tokens / 128 + d->seqs) * d->heads < ((int64_t)1 << 32) / 512, IOS_E_UNSUPPORTED, "too many queries and heads");
+    need((q->tokens / 64 + d->seqs) * d->heads < ((int64_t)1 << 32) / 512, IOS_E_UNSUPPORTED, "too many queries and heads");
     const int splits = usable(prompt_splits(*d, q->tokens), q->tokens, *d, work, work_bytes);
     launched(launch_attn_prompt(*d, *q, *k, *v, *out, lse, cu_q, cu_k, work, splits, (hipStream_t)hip_stream),
              "ios_attn_prompt");
