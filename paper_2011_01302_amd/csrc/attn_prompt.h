@@ -20,14 +20,38 @@ struct PromptArgs {
 };
 
 #if defined(__HIPCC__)
-// The workgroup's head and its tile of a.rows queries: sequence i has tiles from cu_q[i] / rows + i on.  All heads' last
-// tiles, which see most keys, go first (with a whole head after the other, the last head's longest tile began when the
-// others' were done: a third of the time of 8192 causal tokens), and heads that share keys go to one XCD (workgroups
-// go to the eight in turn), whose L2 they share.
-__device__ __forceinline__ int prompt_block(const PromptArgs &a, int64_t *tile) {
+// The head, sequence and first query of this workgroup; false: none.  Heads that share keys go to one XCD (workgroups
+// go to the eight in turn), whose L2 they share.  All heads' longest tiles go first: with a whole head after the other,
+// the last head's longest tile began when the others were done, a third of the time of 8192 causal tokens.  The last
+// tiles of a sequence see most keys; of up to 64 sequences (a lane each) those with most keys come first, more are
+// taken from the last one on.
+__device__ __forceinline__ bool prompt_block(const PromptArgs &a, int *head, int *seq, int64_t *q0) {
   const unsigned h = blockIdx.x % a.heads;
-  *tile = (gridDim.x - 1 - blockIdx.x) / a.heads;
-  return a.heads % 8 ? h : h % 8 * (a.heads / 8) + h / 8;
+  *head = a.heads % 8 ? h : h % 8 * (a.heads / 8) + h / 8;
+  int64_t x = blockIdx.x / a.heads;
+  if (a.seqs > 64) {
+    x = gridDim.x / a.heads - 1 - x;
+    // sequence i has tiles from cu_q[i] / rows + i on
+    auto start = [&](int i) { return clip(a.cu_q[i], a.q.tokens) / a.rows + i; };
+    *seq = find_owner(a.seqs, x, start);
+    *q0 = (x - start(*seq)) * a.rows;
+    return true;
+  }
+  const int lane = threadIdx.x & 63, i = min(lane, a.seqs - 1);
+  const int64_t lq = clip(a.cu_q[i + 1], a.q.tokens) - clip(a.cu_q[i], a.q.tokens);
+  const int lk = (int)(clip(a.cu_k[i + 1], a.k.tokens) - clip(a.cu_k[i], a.k.tokens));
+  const int tiles = lane < a.seqs && lq > 0 ? (int)((lq + a.rows - 1) / a.rows) : 0;
+  int before = 0;
+  for (int j = 0; j < a.seqs; ++j) {
+    const int k = __builtin_amdgcn_readlane(lk, j), t = __builtin_amdgcn_readlane(tiles, j);
+    before += k > lk || (k == lk && j < lane) ? t : 0;
+  }
+  const uint64_t mine = __ballot(x >= before && x < (int64_t)before + tiles);
+  if (mine == 0) return false;
+  const int own = __builtin_ctzll(mine);
+  *seq = own;
+  *q0 = (int64_t)(__builtin_amdgcn_readlane(before, own) + __builtin_amdgcn_readlane(tiles, own) - 1 - (int)x) * a.rows;
+  return true;
 }
 #endif
 

@@ -86,16 +86,14 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
   auto &lds = stage[group];
   const int half = lane >> 5, l31 = lane & 31, l15 = lane & 15;
 
-  int64_t x;
-  const int head = prompt_block(a, &x);
-  auto start = [&](int i) { return clip(a.cu_q[i], a.q.tokens) / kBM + i; };
-  const int seq = find_owner(a.seqs, x, start);
+  int head, seq;
+  int64_t first_query;
+  if (!prompt_block(a, &head, &seq, &first_query)) return;
   const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
   const int lq = (int)(clip(a.cu_q[seq + 1], a.q.tokens) - qa);
   const int lk = max((int)(clip(a.cu_k[seq + 1], a.k.tokens) - ka), 0);
-  const int64_t tile = x - start(seq);
-  if (tile * kBM >= lq) return;
-  const int q0 = (int)tile * kBM, r0 = q0 + 32 * wave;
+  if (first_query >= lq) return;
+  const int q0 = (int)first_query, r0 = q0 + 32 * wave;
   const int kvh = head / a.ratio;
 
   // last key that a row sees (-1: none); rows past the sequence see what its last row sees

@@ -26,16 +26,14 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
   float *sk = stage[group][0], *sv = stage[group][1];
   const int half = lane >> 5, l31 = lane & 31;
 
-  int64_t x;
-  const int head = prompt_block(a, &x);
-  auto start = [&](int i) { return clip(a.cu_q[i], a.q.tokens) / kBM + i; };
-  const int seq = find_owner(a.seqs, x, start);
+  int head, seq;
+  int64_t first_query;
+  if (!prompt_block(a, &head, &seq, &first_query)) return;
   const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
   const int lq = (int)(clip(a.cu_q[seq + 1], a.q.tokens) - qa);
   const int lk = max((int)(clip(a.cu_k[seq + 1], a.k.tokens) - ka), 0);
-  const int64_t tile = x - start(seq);
-  if (tile * kBM >= lq) return;
-  const int q0 = (int)tile * kBM, r0 = q0 + 32 * wave;
+  if (first_query >= lq) return;
+  const int q0 = (int)first_query, r0 = q0 + 32 * wave;
   const int kvh = head / a.ratio;
   const int64_t diff = (int64_t)lk - lq;
   auto last_key = [&](int row) { return a.causal ? (int)min((int64_t)min(row, lq - 1) + diff, (int64_t)lk - 1) : lk - 1; };
