@@ -54,9 +54,8 @@ struct Quant {
   uint32_t param;             // s | z << 16
 };
 template <class T>
-__device__ __forceinline__ Quant quantise(const T *src) {
+__device__ __forceinline__ Quant quantise(const Row8<T> &r) {
   float x[8], lo = kLimit, hi = -kLimit;
-  const Row8<T> r = *(const Row8<T> *)src;
   int nan = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -75,12 +74,19 @@ __device__ __forceinline__ Quant quantise(const T *src) {
   float step = (hi - lo) * (float)(1.0 / 15.0);
   asm("" : "+v"(step));       // rounded to f32 before f16: the compiler may otherwise multiply and convert in one step
   const _Float16 z = (_Float16)lo, s = (_Float16)step;
-  const float fz = (float)z, fs = (float)s;
+  // (x - z) / s as the division rounds it, from the rounded reciprocal: each step takes the exact remainder (one fused
+  // operation) times the reciprocal; the first makes the quotient one of the two nearest numbers, the second the nearest
+  // (Markstein, 1990).  5 operations a value, a division takes 11.
+  const float fz = (float)z, fs = (float)s, inv = 1.f / fs;
   Quant q{0, 0};
   if (!nan) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float c = fs > 0.f ? fminf(fmaxf(rintf((x[e] - fz) / fs), 0.f), 15.f) : 0.f;
+      const float t = x[e] - fz;
+      float v = t * inv;
+      v = fmaf(fmaf(-v, fs, t), inv, v);
+      v = fmaf(fmaf(-v, fs, t), inv, v);
+      const float c = fs > 0.f ? fminf(fmaxf(rintf(v), 0.f), 15.f) : 0.f;
       q.word |= (uint32_t)c << nibble_shift(e);
     }
     q.param = __builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, z) << 16;
@@ -98,17 +104,27 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, ios_toke
   const int tid = threadIdx.x, head = blockIdx.y;
   int seq;
   const TileJob j = find_tile(c, tile_bytes(G), n, seqs, cu, k.tokens, head, &seq);
-  if (!j.tile) return;
+  if (!j.tile || j.lo >= j.hi) return;
+  // every load first: the tokens' values (a thread has up to N octets of K and of V) and the tile, if it holds some
+  constexpr int N = (kTileKeys * 4 * G + 255) / 256;
+  Row8<T> kr[N], vr[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int o = tid + 256 * u, key = min(max(o / (4 * G), j.lo), j.hi - 1), oct = o % (4 * G);
+    const int64_t row = j.row + key;
+    kr[u] = *(const Row8<T> *)((const T *)k.data + row * k.token_stride + head * k.head_stride + oct * 8);
+    vr[u] = *(const Row8<T> *)((const T *)v.data + row * v.token_stride + head * v.head_stride + oct * 8);
+  }
   uintx4 *gt = (uintx4 *)j.tile, *li = (uintx4 *)img;
   for (int i = tid; i < tile_bytes(G) / 16; i += 256) li[i] = j.lo > 0 ? gt[i] : uintx4{0, 0, 0, 0};
   __syncthreads();
-  for (int o = tid; o < kTileKeys * 4 * G; o += 256) {
-    const int key = o / (4 * G), oct = o % (4 * G), g = oct / 4, q = oct % 4;
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int o = tid + 256 * u, key = o / (4 * G), oct = o % (4 * G), g = oct / 4, q = oct % 4;
     if (key < j.lo || key >= j.hi) continue;                 // the 4 lanes of a group agree
-    const int64_t row = j.row + key;
-    const Quant a = quantise((const T *)k.data + row * k.token_stride + head * k.head_stride + oct * 8);
+    const Quant a = quantise(kr[u]);
     img[k_word(G, key, q, g)] = a.word;
-    const Quant b = quantise((const T *)v.data + row * v.token_stride + head * v.head_stride + oct * 8);
+    const Quant b = quantise(vr[u]);
     vc[o] = b.word;
     if (q == 0) {
       ((uint16_t *)img)[k_scale(G, g, key)] = (uint16_t)a.param;

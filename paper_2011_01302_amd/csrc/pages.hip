@@ -87,9 +87,12 @@ __global__ __launch_bounds__(kScanThreads) void cache_reserve_kernel(ios_cache c
   __shared__ int red[kScanThreads / 64];
   const int tid = threadIdx.x;
   const PageWork w(c);
+  // nothing that it reads changes before the last step; each thread keeps its first sequence's
+  const Need own = tid < n ? need_of(c, lg, seqs, add, tid) : Need{-1, 0, 0, -1, 0, 0};
+  auto of = [&](int i) { return i == tid ? own : need_of(c, lg, seqs, add, i); };
   // which sequences share their last page, and which of them comes last
   for (int i = tid; i < n; i += kScanThreads) {
-    const Need d = need_of(c, lg, seqs, add, i);
+    const Need d = of(i);
     if (d.shared >= 0) {
       w.count[d.shared] = 0;
       w.last[d.shared] = -1;
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(kScanThreads) void cache_reserve_kernel(ios_cache c
   }
   __syncthreads();
   for (int i = tid; i < n; i += kScanThreads) {
-    const Need d = need_of(c, lg, seqs, add, i);
+    const Need d = of(i);
     if (d.shared >= 0) {
       atomicAdd(&w.count[d.shared], 1);
       atomicMax(&w.last[d.shared], i);
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(kScanThreads) void cache_reserve_kernel(ios_cache c
     const int i = i0 + tid;
     int need = 0, cp = 0;
     if (i < n) {
-      const Need d = need_of(c, lg, seqs, add, i);
+      const Need d = of(i);
       if (d.slot >= 0) {
         cp = copies(d, i);
         over |= d.new_pages > c.row;
@@ -153,7 +156,7 @@ __global__ __launch_bounds__(kScanThreads) void cache_reserve_kernel(ios_cache c
   for (int i = tid; i < n; i += kScanThreads) {
     // lens, table and refs of this sequence are still as they were: distinct slots, and a shared page's
     // count was compared above
-    const Need d = need_of(c, lg, seqs, add, i);
+    const Need d = of(i);
     if (d.slot < 0) continue;
     int at = w.offs[i];
     const int next = i + 1 < n ? w.offs[i + 1] : total;
