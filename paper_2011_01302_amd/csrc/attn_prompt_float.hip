@@ -10,6 +10,8 @@ namespace {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
+// a row's maximum is only followed when it grows by more than 2^8 (p stays below 2^8)
+constexpr float kSlack = 8.f;
 constexpr int kBM = kFloatRows, kBN = kFloatKeys, kRW = kBM / 32, kGroupThreads = 64 * kRW, KG = 2;
 
 
@@ -91,11 +93,14 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
     for (int p = 0; p < LOADS; ++p) {
       const int s = p * kGroupThreads + tid, r = s / CH, d = s % CH * 4;
       *(floatx4 *)(sk + r * PITCH + d) = nk[p];
-      *(floatx4 *)(sv + r * PITCH + d) = nv[p];
-      bool odd = false;
+      // an infinity or NaN (or four values whose sum is beyond float32): they stay out of the products, see below
+      const float sum = __builtin_fabsf(nv[p][0]) + __builtin_fabsf(nv[p][1]) + __builtin_fabsf(nv[p][2]) + __builtin_fabsf(nv[p][3]);
+      if (!(sum < INFINITY)) {
+        odd_row[r] = 1;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) odd |= !(__builtin_fabsf(nv[p][e]) < INFINITY);
-      if (odd) odd_row[r] = 1;
+        for (int e = 0; e < 4; ++e) nv[p][e] = __builtin_fabsf(nv[p][e]) < INFINITY ? nv[p][e] : 0.f;
+      }
+      *(floatx4 *)(sv + r * PITCH + d) = nv[p];
     }
     __syncthreads();
     if (t + KG < tiles) load(t + KG);
@@ -117,43 +122,51 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
     float mx = s[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32)) * mul;
-    if (__any(mx > m)) {
-      const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+    mx *= mul;
+    if (__any(mx > m + kSlack)) {
+      // each row by its own scores alone, so that no row's result depends on another's
+      const float rm = fmaxf(mx, __shfl_xor(mx, 32)), mn = rm > m + kSlack ? rm : m;
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= f;
 #pragma unroll
       for (int i = 0; i < DB; ++i) o[i] *= f;
     }
     const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
+    auto weight = [&](int r) {
       s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, -mu));
       l += s[r];
-    }
-    // Infinities and NaN of a key that only some rows see are kept out of the product (0 times one of them is a NaN)
-    // and added where they are seen.
-    const bool odd = masked && __any(odd_row[l31]);
+    };
+    float vf[3][DB];                                         // values of keys on their way from LDS
+    auto fetch = [&](int r) {
+#pragma unroll
+      for (int i = 0; i < DB; ++i) vf[r % 3][i] = sv[((r & 3) + 8 * (r >> 2) + 4 * half) * PITCH + 32 * i + l31];
+    };
+    fetch(0);
+    fetch(1);
+    weight(0);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int key = (r & 3) + 8 * (r >> 2) + 4 * half;
+      if (r + 2 < 16) fetch(r + 2);
+      if (r + 1 < 16) weight(r + 1);
 #pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        float vf = sv[key * PITCH + 32 * i + l31];
-        if (odd) vf = __builtin_fabsf(vf) < INFINITY ? vf : 0.f;
-        o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[r], o[i], 0, 0, 0);
-      }
+      for (int i = 0; i < DB; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r % 3][i], s[r], o[i], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (odd) {
+    // The infinities and NaN that were left out (0 times one of them is a NaN, also for rows that do not see the key):
+    // added to the rows that see them.
+    if (__any(odd_row[l31])) {
       for (int key = 0; key < kBN; ++key) {
         if (!__builtin_amdgcn_readfirstlane(odd_row[key])) continue;
         const bool seen = t * kBN + key <= lim;
+        const float *src = vbase + (int64_t)(t * kBN + key) * a.v.token_stride;
 #pragma unroll
         for (int i = 0; i < DB; ++i)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float vf = sv[key * PITCH + 32 * i + (r & 3) + 8 * (r >> 2) + 4 * half];
-            if (seen && !(__builtin_fabsf(vf) < INFINITY)) o[i][r] += vf;
+            const int d = 32 * i + (r & 3) + 8 * (r >> 2) + 4 * half;
+            const float x = d < a.dim ? src[d] : 0.f;
+            if (seen && !(__builtin_fabsf(x) < INFINITY)) o[i][r] += x;
           }
       }
     }
