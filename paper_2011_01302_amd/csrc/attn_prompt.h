@@ -20,6 +20,11 @@ struct PromptArgs {
 };
 
 #if defined(__HIPCC__)
+constexpr uint32_t kOutside = 0x80000000u;       // byte offset past every buffer: reads as 0
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, 0x7FFFFFFF, 0x00020000);
+}
+
 // The head, sequence and first query of this workgroup; false: none.  Heads that share keys go to one XCD (workgroups
 // go to the eight in turn), whose L2 they share.  All heads' longest tiles go first: with a whole head after the other,
 // the last head's longest tile began when the others were done, a third of the time of 8192 causal tokens.  The last

@@ -32,7 +32,6 @@ constexpr int kFewBlocks = 129, kPartKeys = 256, kTwoGroups = 320;
 // p = 2^(score - m), m kTop below the row's largest score when it was last followed, which it is when a score passes it
 // by kTop + 2 (sums are in 32 bits).  f16 then holds p from 2^15 down to 2^-38 of the largest.
 template <class T> constexpr float kTop = std::is_same_v<T, _Float16> ? 13.f : 0.f;
-constexpr uint32_t kOutside = 0x80000000u;       // byte offset past every buffer: reads as 0
 
 template <class T>
 __device__ __forceinline__ floatx16 mfma(shortx8 a, shortx8 b, floatx16 c) {
@@ -54,9 +53,6 @@ __device__ __forceinline__ int swz_v(int r) {
   return DP == 128 ? 4 * (r & 3) : DP == 64 ? 4 * (r >> 1 & 1) : 0;
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *p) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, 0x7FFFFFFF, 0x00020000);
-}
 // Direct global -> LDS load of 16 bytes a lane, l the same for every lane; the
 // compiler does not see the write (readers wait for vmcnt(0) and a barrier).
 __device__ __forceinline__ void lds_copy16(__amdgpu_buffer_rsrc_t r, unsigned char *l, uint32_t off) {

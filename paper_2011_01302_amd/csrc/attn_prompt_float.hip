@@ -15,6 +15,10 @@ constexpr float kSlack = 8.f;
 constexpr int kBM = kFloatRows, kBN = kFloatKeys, kRW = kBM / 32, kGroupThreads = 64 * kRW, KG = 2;
 
 
+__device__ __forceinline__ floatx4 load16(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+  return __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
+}
+
 // Two waves of 32 queries, and two groups of such waves that take the tiles in turn and are joined at the end: the
 // matrix cores are what bounds, so the work is cut small enough to come out even over them.
 template <int DP>
@@ -71,16 +75,23 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
 #pragma unroll
   for (int i = 0; i < DB; ++i) o[i] = zero;
 
+  // what this thread loads of a tile, through descriptors (past their end, and past the sequence's last key, reads as 0)
+  uint32_t koff[LOADS], voff[LOADS];
+#pragma unroll
+  for (int p = 0; p < LOADS; ++p) {
+    const int s = p * kGroupThreads + tid, r = s / CH, d = s % CH * 4;
+    koff[p] = d < a.dim ? (uint32_t)(r * (int)a.k.token_stride + d) * 4 : kOutside;
+    voff[p] = d < a.dim ? (uint32_t)(r * (int)a.v.token_stride + d) * 4 : kOutside;
+  }
   floatx4 nk[LOADS], nv[LOADS];                              // the next tile, on its way
   auto load = [&](int t) {
+    const __amdgpu_buffer_rsrc_t kr = buffer(kbase + (int64_t)t * kBN * a.k.token_stride);
+    const __amdgpu_buffer_rsrc_t vr = buffer(vbase + (int64_t)t * kBN * a.v.token_stride);
 #pragma unroll
     for (int p = 0; p < LOADS; ++p) {
-      const int s = p * kGroupThreads + tid, r = s / CH, d = s % CH * 4;
-      nk[p] = nv[p] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (t * kBN + r < lk && d < a.dim) {
-        nk[p] = *(const floatx4 *)(kbase + (int64_t)(t * kBN + r) * a.k.token_stride + d);
-        nv[p] = *(const floatx4 *)(vbase + (int64_t)(t * kBN + r) * a.v.token_stride + d);
-      }
+      const bool in = t * kBN + (p * kGroupThreads + tid) / CH < lk;
+      nk[p] = load16(kr, in ? koff[p] : kOutside);
+      nv[p] = load16(vr, in ? voff[p] : kOutside);
     }
   };
   if (t0 + group < tiles) load(t0 + group);
@@ -159,14 +170,16 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
       for (int key = 0; key < kBN; ++key) {
         if (!__builtin_amdgcn_readfirstlane(odd_row[key])) continue;
         const bool seen = t * kBN + key <= lim;
-        const float *src = vbase + (int64_t)(t * kBN + key) * a.v.token_stride;
+        const float *src = vbase + (int64_t)(t * kBN + key) * a.v.token_stride + 4 * half;
 #pragma unroll
         for (int i = 0; i < DB; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int d = 32 * i + (r & 3) + 8 * (r >> 2) + 4 * half;
-            const float x = d < a.dim ? src[d] : 0.f;
-            if (seen && !(__builtin_fabsf(x) < INFINITY)) o[i][r] += x;
+          for (int r4 = 0; r4 < 4; ++r4) {
+            if (32 * i + 8 * r4 + 4 * half >= a.dim) continue;
+            const floatx4 x = *(const floatx4 *)(src + 32 * i + 8 * r4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (seen && !(__builtin_fabsf(x[e]) < INFINITY)) o[i][4 * r4 + e] += x[e];
           }
       }
     }
