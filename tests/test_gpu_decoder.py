@@ -754,3 +754,21 @@ def test_forked_sequences_keep_their_tokens():
             assert equal(gk, held(torch.cat([k, tail]))) and equal(gv, held(torch.cat([v, tail])))
         gk, _ = c.read([2], [1], layer=layer)
         assert equal(gk, held(new[2][2:3]))
+
+
+def test_example_answers():
+    """The example's path, end to end: answers differ, sharing holds, and the cache's prompt is what was written."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "answer_maps.py")
+    spec = importlib.util.spec_from_file_location("answer_maps", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    ids, pages, dec = ex.answers(3, 8)
+    assert [len(r) for r in ids] == [8] * 3 and len({r[0] for r in ids}) == 3
+    prompt, page = 1225, ex.PAGE
+    own = -(-(prompt + 7) // page) - prompt // page          # pages that an answer does not share
+    assert pages == [-(-prompt // page) + 3 * own, -(-prompt // page) + own]
+    assert dec.lens.tolist() == [prompt, prompt + 7, 0, 0]
+    assert sorted(set(dec.table[dec.table >= 0].tolist())) == list(range(pages[1]))
+    assert ids == ex.answers(3, 8)[0]                        # the same again
