@@ -40,7 +40,7 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs &a, int *head, int
     auto start = [&](int i) { return clip(a.cu_q[i], a.q.tokens) / a.rows + i; };
     *seq = find_owner(a.seqs, x, start);
     *q0 = (x - start(*seq)) * a.rows;
-    return true;
+    return *q0 >= 0;                                              // rows before the first sequence, offsets that descend
   }
   const int lane = threadIdx.x & 63, i = min(lane, a.seqs - 1);
   const int64_t lq = clip(a.cu_q[i + 1], a.q.tokens) - clip(a.cu_q[i], a.q.tokens);

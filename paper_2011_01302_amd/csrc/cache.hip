@@ -39,7 +39,7 @@ __device__ __forceinline__ TileJob find_tile(const CacheView &c, int tile_b, int
   const int64_t first = (int64_t)len - (b - a);              // position of the call's first token
   const int64_t p0 = first < 0 ? 0 : first;
   const int64_t t0 = (p0 / kTileKeys + (blockIdx.x - start(i))) * kTileKeys;
-  if (b <= a || t0 >= len) return j;
+  if (b <= a || blockIdx.x < start(i) || t0 >= len) return j;  // units before the first sequence, offsets that descend
   j.tile = cache_tile(c, slot, (int)t0, head, tile_b);
   j.lo = p0 > t0 ? (int)(p0 - t0) : 0;
   j.hi = len - t0 < kTileKeys ? (int)(len - t0) : kTileKeys;

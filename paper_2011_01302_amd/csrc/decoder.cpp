@@ -1,6 +1,7 @@
 // Entry points of the decoder operators (declared and documented in ios.h):
 // every size, pointer and alignment that the host can see is checked here,
 // before anything is launched.
+#include <cmath>
 #include <cstring>
 #include <new>
 
@@ -73,6 +74,7 @@ void check_desc(const ios_attn_desc *d) {
   need(d->seqs >= 1 && d->seqs <= kMaxAttnSeqs, IOS_E_ARG, "seqs out of range");
   need(d->causal == 0 || d->causal == 1, IOS_E_ARG, "causal must be 0 or 1");
   need(d->max_keys >= 0, IOS_E_ARG, "negative max_keys");
+  need(std::isfinite(d->scale), IOS_E_ARG, "scale must be finite");
 }
 
 // The cache's sizes; `state`: its pointers too.

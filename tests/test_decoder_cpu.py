@@ -41,7 +41,8 @@ def refused(name, f, *a):
     ("IOS_E_ARG", dict(dtype=3)), ("IOS_E_ARG", dict(dtype=-1)), ("IOS_E_ARG", dict(heads=0)),
     ("IOS_E_ARG", dict(kv_heads=0)), ("IOS_E_SHAPE", dict(heads=9)), ("IOS_E_UNSUPPORTED", dict(head_dim=60)),
     ("IOS_E_UNSUPPORTED", dict(head_dim=136)), ("IOS_E_ARG", dict(head_dim=0)), ("IOS_E_ARG", dict(seqs=0)),
-    ("IOS_E_ARG", dict(seqs=65536)), ("IOS_E_ARG", dict(causal=2)), ("IOS_E_ARG", dict(max_keys=-1))])
+    ("IOS_E_ARG", dict(seqs=65536)), ("IOS_E_ARG", dict(causal=2)), ("IOS_E_ARG", dict(max_keys=-1)),
+    ("IOS_E_ARG", dict(scale=float("nan"))), ("IOS_E_ARG", dict(scale=float("inf")))])
 def test_attention_descriptor(name, kw):
     d = desc(**kw)
     refused(name, I.ios_attn_work_bytes, d, 10)

@@ -260,6 +260,27 @@ def test_prompt_many_sequences():
         check(out[o[i]:o[i] + m, 0], ref, a, g, 2.0 ** -11, 2.0 ** -11, m)
 
 
+@pytest.mark.parametrize("typ", ["f16", "f32"])
+@pytest.mark.parametrize("n", [3, 100])
+def test_prompt_offsets_that_start_later(typ, n):
+    """The first sequence begins behind rows that belong to none."""
+    dt, lens, skip = TYPES[typ][0], [1 + 3 * (i % 7) for i in range(n)], 300
+    total = skip + sum(lens)
+    q, k, v = (randn((total, 2, 32), dt, s) for s in (1, 2, 3))
+    d = desc(typ, 2, 2, 32, n, 1, 32)
+    out = torch.full_like(q, 7.0)
+    o = [skip + x for x in offsets(lens)]
+    cu = i32(o)
+    I.ios_attn_prompt(d, toks(q), toks(k), toks(v), toks(out), 0, cu.data_ptr(), cu.data_ptr(), 0, 0, stream())
+    torch.cuda.synchronize()
+    assert (out[:skip] == 7).all()
+    for i in range(0, n, 7):
+        ref, a, _, g = attend(q[o[i]:o[i + 1], 1], k[o[i]:o[i + 1], 1], v[o[i]:o[i + 1], 1], d.scale,
+                              causal_mask(lens[i], lens[i], 1))
+        u = TYPES[typ][2]
+        check(out[o[i]:o[i + 1], 1], ref, a, g, u, 0.0 if typ == "f32" else u, lens[i])
+
+
 def test_prompt_bad_offsets_stay_inside():
     """Offsets that leave the tensors or descend are clipped: no fault, and sound sequences keep their results."""
     q, k, v = (randn((200, 2, 64), torch.float16, s) for s in (1, 2, 3))
@@ -427,6 +448,26 @@ def test_cache_append_and_read_edges():
     assert torch.equal(before, c.pool)
     gk, _ = c.read([0], [40])
     assert equal(gk[:32], held(k[5:37])) and (gk[32:] == 0).all()
+
+
+def test_cache_offsets_that_start_later_or_descend():
+    c = Cache(1, 32, 32, 16, 3, 4)
+    c.place([70, 40, 33])
+    k, v = randn((400, 1, 32), torch.float32, 1), randn((400, 1, 32), torch.float32, 2)
+    seqs, cu = i32([0, 1]), i32([200, 270, 310])
+    I.ios_cache_append(c.c, 0, I.IOS_F32, toks(k), toks(v), 2, seqs.data_ptr(), cu.data_ptr(), stream())
+    gk, gv = c.read([0, 1], [70, 40])
+    assert equal(gk, held(k[200:310])) and equal(gv, held(v[200:310]))
+    out = torch.full_like(k, 9.0)
+    I.ios_cache_read(c.c, 0, I.IOS_F32, toks(out), toks(out.clone()), 2, seqs.data_ptr(), cu.data_ptr(), stream())
+    torch.cuda.synchronize()
+    assert (out[:200] == 9).all() and equal(out[200:310], held(k[200:310])) and (out[310:] == 9).all()
+    before = c.pool.clone()
+    for bad in ([390, 100, 50], [10 ** 9, -5, -9], [400, 400, 0]):
+        cu = i32(bad)
+        I.ios_cache_append(c.c, 0, I.IOS_F32, toks(k), toks(v), 2, seqs.data_ptr(), cu.data_ptr(), stream())
+    torch.cuda.synchronize()
+    assert torch.equal(before, c.pool)
 
 
 def test_cache_append_strides():
