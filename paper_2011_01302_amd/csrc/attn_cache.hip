@@ -7,6 +7,13 @@
 // range of the sequence; its eight waves take tiles of 32 keys in turn and are
 // joined at the end, the ranges in a second launch.
 //
+// 32 sequences of 8192 .. 32031 tokens, 8 heads of 128, 4 queries each: 823 MB in
+// 175 us, 4.7 TB/s (a large copy moves 4.95); the loads alone take 152 us.  One
+// sequence of 131072 tokens and 2 such heads: 14 us, and 4 for the join.  Tiles
+// reach LDS through a ring of direct copies per wave, two tiles deep: with
+// 16 waves a CU about 80 KB are on their way, and no barrier is needed before
+// the end (registers and no ring: 595 us; four waves and three tiles: 220).
+//
 // Scores are exact up to 32-bit sums: with q summed over the values of a
 // group, s . (z + s_k c) = z sum(q) + s_k (c . q), c exact in f16 and q too
 // (bf16 after scaling a row by a power of two; float32 as two f16 parts).

@@ -8,6 +8,13 @@
 // need one exchange between the two half waves, and the scores are the second
 // product's operand as they stand (keys 8 i + 4 h + 0 .. 3 of a tile lie in
 // half h; V is read in that order).
+//
+// Bound by the matrix rate and the power behind it for heads of 96 and 128
+// (16384 causal tokens, 32 heads of 128: 2.03 ms, 1080 TFLOP/s, where a large
+// matrix product of the library reaches 1130), by the exponentials and the
+// other vector instructions of the softmax for smaller heads (4096 causal
+// tokens, 16 heads of 64: 60 us, 570 TFLOP/s), by its longest rows where
+// prompts of different lengths are packed.
 #include <type_traits>
 
 #include "attn_prompt.h"
@@ -27,8 +34,11 @@ typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
 constexpr int kBM = kRows, kBN = kKeys;
 // Fewer than kFewBlocks workgroups: the keys of a row are spread over workgroups (a second launch joins them), in parts
-// of at least kPartKeys keys.  Up to kTwoGroups: over two groups of waves of one workgroup.
-constexpr int kFewBlocks = 129, kPartKeys = 256, kTwoGroups = 320;
+// of at least kPartKeys keys (32 heads of 128: 1 row over 6000 keys 28 us, 108 in one part).  Up to kTwoGroups
+// workgroups, and from kTwoKeys keys on: over two groups of waves of one workgroup (2048 causal tokens, 16 heads of 64,
+// 272 workgroups: 26.6 us, 30.5 with one group; 32 heads of 128, 544 workgroups: 57.5 and 53.3; 512 tokens, 160
+// workgroups: 17.5 and 16.7).
+constexpr int kFewBlocks = 129, kPartKeys = 256, kTwoGroups = 320, kTwoKeys = 1024;
 // p = 2^(score - m), m kTop below the row's largest score when it was last followed, which it is when a score passes it
 // by kTop + 2 (sums are in 32 bits).  f16 then holds p from 2^15 down to 2^-38 of the largest.
 template <class T> constexpr float kTop = std::is_same_v<T, _Float16> ? 13.f : 0.f;
@@ -53,8 +63,8 @@ __device__ __forceinline__ int swz_v(int r) {
   return DP == 128 ? 4 * (r & 3) : DP == 64 ? 4 * (r >> 1 & 1) : 0;
 }
 
-// Direct global -> LDS load of 16 bytes a lane, l the same for every lane; the
-// compiler does not see the write (readers wait for vmcnt(0) and a barrier).
+// Direct global -> LDS load of 16 bytes a lane, l the same for every lane
+// (readers wait for vmcnt(0) and a barrier).
 __device__ __forceinline__ void lds_copy16(__amdgpu_buffer_rsrc_t r, unsigned char *l, uint32_t off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)l, 16, (int)off, 0, 0, 0);
 }
@@ -498,7 +508,7 @@ hipError_t launch_attn_prompt(const ios_attn_desc &d, const ios_tokens &q, const
     const hipError_t e = launch_attn_prompt_float(a, splits, s);
     return e == hipSuccess ? join<float>(a, splits, s) : e;
   }
-  const bool two = splits == 1 && prompt_blocks(d, q.tokens) <= kTwoGroups;
+  const bool two = splits == 1 && d.max_keys >= kTwoKeys && prompt_blocks(d, q.tokens) <= kTwoGroups;
   return d.dtype == IOS_F16 ? for_dim<_Float16>(a, two, splits, s) : for_dim<__bf16>(a, two, splits, s);
 }
 

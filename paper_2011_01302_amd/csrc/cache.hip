@@ -4,7 +4,9 @@
 // LDS: the V codes of 8 tokens share a word, so a tile is the smallest piece
 // that is written whole.  Where the tile already holds earlier tokens it is
 // read first.  Both calls are bound by memory: 2 D values in and 5/4 D bytes
-// out per token and head.
+// out per token and head.  35472 tokens of 8 heads of 128: append 52 .. 66 us
+// (190 MB), read as float32 63 us (336 MB, 5.3 TB/s); 32 single tokens 5.5 and
+// 3.7 us, a chain of dependent loads (offsets, slot, length, page, values).
 #include "decoder.h"
 
 namespace ios {
