@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
   const int64_t diff = (int64_t)lk - lq;
   auto last_key = [&](int row) { return a.causal ? (int)min((int64_t)min(row, lq - 1) + diff, (int64_t)lk - 1) : lk - 1; };
   const int lim = max(last_key(r0 + l31), -1);
-  const int lim_lo = last_key(r0), lim_hi = last_key(r0 + 31);
+  const int lim_lo = last_key(r0), lim_hi = r0 < lq ? last_key(r0 + 31) : -1;   // waves past the sequence sit out
   int tiles = max(last_key(q0 + kBM - 1) + kBN, 0) / kBN;
   const int split = blockIdx.z, t0 = split * a.chunk;
   if (a.part) {
