@@ -34,7 +34,7 @@ typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
 constexpr int kBM = kRows, kBN = kKeys;
 // Fewer than kFewBlocks workgroups: the keys of a row are spread over workgroups (a second launch joins them), in parts
-// of at least kPartKeys keys (32 heads of 128: 1 row over 6000 keys 28 us, 108 in one part).  Up to kTwoGroups
+// of at least kPartKeys keys (32 heads of 128: 1 row over 6000 keys 18 us, 96 in one part).  Up to kTwoGroups
 // workgroups, and from kTwoKeys keys on: over two groups of waves of one workgroup (2048 causal tokens, 16 heads of 64,
 // 272 workgroups: 26.6 us, 30.5 with one group; 32 heads of 128, 544 workgroups: 57.5 and 53.3; 512 tokens, 160
 // workgroups: 17.5 and 16.7).
