@@ -373,12 +373,12 @@ template <class T, int G>
 __global__ __launch_bounds__(256) void attn_join_kernel(CacheView c, int heads, int splits, int chunk, ios_tokens out,
                                                         float *lse, const int32_t *seqs, const float *part) {
   const int64_t i = blockIdx.x / heads, h = blockIdx.x % heads;
-  join_parts<T>(blockIdx.x, out.tokens * heads, 32 * G, splits, part,
-                [&] {
-                  const int tiles = (cache_len(c, seqs[i]) + kTileKeys - 1) / kTileKeys;
-                  return min((tiles + chunk - 1) / chunk, splits);
-                },
-                (T *)out.data + i * out.token_stride + h * out.head_stride, lse ? lse + h * out.tokens + i : nullptr);
+  join_parts<T, false>(blockIdx.x, out.tokens * heads, 32 * G, splits, part,
+                       [&] {
+                         const int tiles = (cache_len(c, seqs[i]) + kTileKeys - 1) / kTileKeys;
+                         return min((tiles + chunk - 1) / chunk, splits);
+                       },
+                       (T *)out.data + i * out.token_stride + h * out.head_stride, lse ? lse + h * out.tokens + i : nullptr);
 }
 
 int64_t keys_of(const ios_attn_desc &d) { return d.max_keys ? d.max_keys : 1 << 16; }

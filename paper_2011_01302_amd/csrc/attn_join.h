@@ -1,7 +1,8 @@
 // Joining the parts of attention rows whose keys were spread over workgroups.
 //
-// Part s of a row leaves in the workspace sum_j p_j v_j ([row][part][dim] floats), and behind all of those its
-// reference m and the sum of p_j = 2^(score_j - m) ([row][part][2]).
+// Part s of a row leaves in the workspace sum_j p_j v_j ([row][part][dim] floats), or that divided by sum_j p_j (`kMeans`:
+// values may reach to float32's largest, and sums of them not), and behind all of those its reference m and the sum of
+// p_j = 2^(score_j - m) ([row][part][2]).
 #pragma once
 
 #include "decoder.h"
@@ -15,7 +16,7 @@ constexpr int kMaxParts = 128;
 // One workgroup of 256 threads joins row `row` of `rows`: weights of the parts first (a thread each), then four values
 // a thread, the parts spread over the threads; every sum in a fixed order.  The first loads do not wait for the number
 // of parts that hold anything (count()); the others' values are left out.
-template <class T, class F>
+template <class T, bool kMeans, class F>
 __device__ __forceinline__ void join_parts(int64_t row, int64_t rows, int dim, int splits, const float *part, F count,
                                            T *out, float *lse) {
   static_assert(kMaxParts <= 256, "a thread per part");
@@ -41,12 +42,17 @@ __device__ __forceinline__ void join_parts(int64_t row, int64_t rows, int dim, i
   mm = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   const float mu = mm == -INFINITY ? 0.f : mm, f = tid < n ? __builtin_amdgcn_exp2f(m0 - mu) : 0.f;
   float ll = tid < n ? f * l0 : 0.f;
-  if (tid < kMaxParts) weight[tid] = f;
+  if (!kMeans && tid < kMaxParts) weight[tid] = f;
+  const float fl = ll;
 #pragma unroll
   for (int y = 1; y < 64; y <<= 1) ll += __shfl_xor(ll, y);
   if (lane == 0) red[1][wave] = ll;
   __syncthreads();
   ll = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+  if constexpr (kMeans) {                                         // the parts' shares: they sum to 1
+    if (tid < kMaxParts) weight[tid] = ll == 0.f ? 0.f : fl / ll;
+    __syncthreads();
+  }
   floatx4 v = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = w; s0 < n; s0 += 8 * W) {
     if (s0 != w) load(s0);
@@ -60,7 +66,7 @@ __device__ __forceinline__ void join_parts(int64_t row, int64_t rows, int dim, i
     for (int y = 1; y < W; ++y) v += sum[tid + y * Q];
     struct alignas(4 * sizeof(T)) { T v[4]; } r;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r.v[e] = (T)(ll == 0.f ? 0.f : v[e] / ll);
+    for (int e = 0; e < 4; ++e) r.v[e] = (T)(kMeans ? v[e] : ll == 0.f ? 0.f : v[e] / ll);
     *(decltype(r) *)(out + 4 * tid) = r;
   }
   if (lse && tid == 0) *lse = (mm + __builtin_log2f(ll)) * kLn2;

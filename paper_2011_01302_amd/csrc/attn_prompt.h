@@ -20,6 +20,11 @@ struct PromptArgs {
 };
 
 #if defined(__HIPCC__)
+// bf16 and float32 values reach to float32's largest, and weights to 2^8: where a row's sum leaves the range, the keys
+// are walked again with weights times kDown (a power of two: every other result stays as it was, to the bit, unless it
+// is below 2^-86).  2^28 keys then stay within the range.
+constexpr float kDown = 0x1p-40f, kUp = 0x1p40f;
+
 constexpr uint32_t kOutside = 0x80000000u;       // byte offset past every buffer: reads as 0
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *p) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, 0x7FFFFFFF, 0x00020000);

@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
       for (int i = 0; i < DB; ++i) o[i] *= f;
     }
   };
-  auto weights = [&](const floatx16 *s, shortx8 *pf) {
+  auto weights = [&](const floatx16 *s, shortx8 *pf, float by) {
     const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
       for (int r = 0; r < 16; ++r) {
         const float e = __builtin_amdgcn_exp2f(fmaf(s[b][r], mul, -mu));
         l += e;
-        pf[2 * b + (r >> 3)][r & 7] = __builtin_bit_cast(short, (T)e);        // p as the inputs' type: 2^-9 (2^-12) each
+        pf[2 * b + (r >> 3)][r & 7] = __builtin_bit_cast(short, (T)(e * by));  // p as the inputs' type: 2^-9 (2^-12) each
       }
   };
   auto values = [&](const unsigned char *sv, int i, int ks) {
@@ -314,69 +314,83 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
       if (t0 + (k + 1) * KG < tiles) step(k + 1, sn, s);
     }
   }
-  int odd = 0;
+  // whether any wave of the workgroup found a number that is not finite
+  auto odd = [&] {
+    int x = 0;
 #pragma unroll
-  for (int i = 0; i < DB; ++i)
+    for (int i = 0; i < DB; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) odd |= !(__builtin_fabsf(o[i][r]) < INFINITY);
-  // whether any wave of the workgroup found one
-  int *found = (int *)stage;
-  __syncthreads();                                           // the tiles are done with
-  odd = __any(odd);
-  if (lane == 0) found[threadIdx.x >> 6] = odd;
-  __syncthreads();
+      for (int r = 0; r < 16; ++r) x |= !(__builtin_fabsf(o[i][r]) < INFINITY);
+    int *found = (int *)stage;
+    __syncthreads();                                         // the tiles are done with
+    x = __any(x);
+    if (lane == 0) found[threadIdx.x >> 6] = x;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 4 * KG; ++w) odd |= found[w];
-  if (__builtin_amdgcn_readfirstlane(odd)) {
-    // Again, with care: infinities and NaN among the values of a tile that not every row sees whole are kept out of the
-    // product (0 times one of them is a NaN) and reach the rows that see them by counts.
-    clear();
-    for (int k = 0; t0 + k * KG < tiles; ++k) {
-      const int t = t0 + k * KG + group;
-      __syncthreads();
-      if (t < tiles) {
-        issue_k(t, 0);
-        issue_v(t, 0);
-      }
-      arrived();
-      if (t >= tiles || t * kBN > lim_hi) continue;
-      floatx16 s[2];
-      shortx8 pf[4];
-      scores(lds[0][0], s);
-      hide(t, s);
-      follow(largest(s));
-      weights(s, pf);
+    for (int w = 0; w < 4 * KG; ++w) x |= found[w];
+    return __builtin_amdgcn_readfirstlane(x);
+  };
+  // Again, with care: infinities and NaN among the values of a tile that not every row sees whole are kept out of the
+  // product (0 times one of them is a NaN) and reach the rows that see them by counts.  And once more if a sum has left
+  // float32's range (f16 values stay far below).  (As a loop over both the kernel for heads of 128 spills registers.)
+  float up = 1.f;
+  if (odd()) {
+    auto careful = [&](float by) {
+      clear();
+      for (int k = 0; t0 + k * KG < tiles; ++k) {
+        const int t = t0 + k * KG + group;
+        __syncthreads();
+        if (t < tiles) {
+          issue_k(t, 0);
+          issue_v(t, 0);
+        }
+        arrived();
+        if (t >= tiles || t * kBN > lim_hi) continue;
+        floatx16 s[2];
+        shortx8 pf[4];
+        scores(lds[0][0], s);
+        hide(t, s);
+        follow(largest(s));
+        weights(s, pf, by);
 #pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        floatx16 nan = zero, up = zero, down = zero;
+        for (int i = 0; i < DB; ++i) {
+          floatx16 nan = zero, up = zero, down = zero;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          shortx8 vf = values(lds[0][1], i, ks);
-          if (masked(t)) {
-            constexpr int inf = std::is_same_v<T, _Float16> ? 0x7C00 : 0x7F80;
-            const short one = __builtin_bit_cast(short, (T)1.f);
-            shortx8 vn, vu, vd, seen;
+          for (int ks = 0; ks < 4; ++ks) {
+            shortx8 vf = values(lds[0][1], i, ks);
+            if (masked(t)) {
+              constexpr int inf = std::is_same_v<T, _Float16> ? 0x7C00 : 0x7F80;
+              const short one = __builtin_bit_cast(short, (T)1.f);
+              shortx8 vn, vu, vd, seen;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int mag = vf[e] & 0x7FFF;
-              vn[e] = mag > inf ? one : 0;
-              vu[e] = vf[e] == inf ? one : 0;
-              vd[e] = mag == inf && vf[e] < 0 ? one : 0;
-              if (mag >= inf) vf[e] = 0;
-              seen[e] = t * kBN + 16 * ks + 4 * half + (e & 3) + 8 * (e >> 2) <= lim ? one : 0;
+              for (int e = 0; e < 8; ++e) {
+                const int mag = vf[e] & 0x7FFF;
+                vn[e] = mag > inf ? one : 0;
+                vu[e] = vf[e] == inf ? one : 0;
+                vd[e] = mag == inf && vf[e] < 0 ? one : 0;
+                if (mag >= inf) vf[e] = 0;
+                seen[e] = t * kBN + 16 * ks + 4 * half + (e & 3) + 8 * (e >> 2) <= lim ? one : 0;
+              }
+              nan = mfma<T>(vn, seen, nan);
+              up = mfma<T>(vu, seen, up);
+              down = mfma<T>(vd, seen, down);
             }
-            nan = mfma<T>(vn, seen, nan);
-            up = mfma<T>(vu, seen, up);
-            down = mfma<T>(vd, seen, down);
+            o[i] = mfma<T>(vf, pf[ks], o[i]);
           }
-          o[i] = mfma<T>(vf, pf[ks], o[i]);
-        }
-        if (masked(t)) {
+          if (masked(t)) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            o[i][r] += nan[r] > 0.f || (up[r] > 0.f && down[r] > 0.f) ? NAN
-                       : up[r] > 0.f ? INFINITY : down[r] > 0.f ? -INFINITY : 0.f;
+            for (int r = 0; r < 16; ++r)
+              o[i][r] += nan[r] > 0.f || (up[r] > 0.f && down[r] > 0.f) ? NAN
+                         : up[r] > 0.f ? INFINITY : down[r] > 0.f ? -INFINITY : 0.f;
+          }
         }
+      }
+    };
+    careful(1.f);
+    if constexpr (!std::is_same_v<T, _Float16>) {
+      if (odd()) {
+        careful(kDown);
+        up = kUp;
       }
     }
   }
@@ -397,13 +411,22 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     __syncthreads();
     if (group == 1) return;
     const float m1 = ml[0], mm = fmaxf(m, m1), mu = mm == -INFINITY ? 0.f : mm;
-    const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(m1 - mu);
+    float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(m1 - mu);
     m = mm;
     l = l * f0 + ml[256] * f1;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    f0 *= inv;
+    f1 *= inv;
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * f0 + oo[(i * 16 + r) * 64] * f1;
+      for (int r = 0; r < 16; ++r) o[i][r] = (o[i][r] * f0 + oo[(i * 16 + r) * 64] * f1) * up;
+  } else {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * inv * up;
   }
   const int row = r0 + l31;
   if (row >= lq) return;
@@ -424,7 +447,6 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     }
     return;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
   T *dst = (T *)a.out.data + (qa + row) * a.out.token_stride + head * a.out.head_stride;
 #pragma unroll
   for (int i = 0; i < DB; ++i)
@@ -434,7 +456,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
       if (d < a.dim) {
         struct alignas(8) { T v[4]; } w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w.v[e] = (T)(o[i][4 * r4 + e] * inv);
+        for (int e = 0; e < 4; ++e) w.v[e] = (T)o[i][4 * r4 + e];
         *(decltype(w) *)(dst + d) = w;
       }
     }
@@ -446,20 +468,20 @@ template <class T>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int splits) {
   const int64_t i = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
   if (i < clip(a.cu_q[0], a.q.tokens) || i >= clip(a.cu_q[a.seqs], a.q.tokens)) return;
-  join_parts<T>(blockIdx.x, a.q.tokens * a.heads, a.dim, splits, a.part,
-                [&] {
-                  // the workgroup's tiles, as the first launch counted them
-                  const int seq = find_row(a.seqs, i, [&](int s) { return clip(a.cu_q[s], a.q.tokens); });
-                  const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
-                  const int64_t lq = clip(a.cu_q[seq + 1], a.q.tokens) - qa;
-                  const int64_t lk = max(clip(a.cu_k[seq + 1], a.k.tokens) - ka, (int64_t)0);
-                  const int64_t row = (i - qa) / a.rows * a.rows + a.rows - 1;
-                  const int64_t last = a.causal ? min(min(row, lq - 1) + lk - lq, lk - 1) : lk - 1;
-                  const int64_t tiles = max(last + a.keys, (int64_t)0) / a.keys;
-                  return (int)min(max((tiles + a.chunk - 1) / a.chunk, (int64_t)1), (int64_t)splits);
-                },
-                (T *)a.out.data + i * a.out.token_stride + h * a.out.head_stride,
-                a.lse ? a.lse + h * a.q.tokens + i : nullptr);
+  join_parts<T, true>(blockIdx.x, a.q.tokens * a.heads, a.dim, splits, a.part,
+                      [&] {
+                        // the workgroup's tiles, as the first launch counted them
+                        const int seq = find_row(a.seqs, i, [&](int s) { return clip(a.cu_q[s], a.q.tokens); });
+                        const int64_t qa = clip(a.cu_q[seq], a.q.tokens), ka = clip(a.cu_k[seq], a.k.tokens);
+                        const int64_t lq = clip(a.cu_q[seq + 1], a.q.tokens) - qa;
+                        const int64_t lk = max(clip(a.cu_k[seq + 1], a.k.tokens) - ka, (int64_t)0);
+                        const int64_t row = (i - qa) / a.rows * a.rows + a.rows - 1;
+                        const int64_t last = a.causal ? min(min(row, lq - 1) + lk - lq, lk - 1) : lk - 1;
+                        const int64_t tiles = max(last + a.keys, (int64_t)0) / a.keys;
+                        return (int)min(max((tiles + a.chunk - 1) / a.chunk, (int64_t)1), (int64_t)splits);
+                      },
+                      (T *)a.out.data + i * a.out.token_stride + h * a.out.head_stride,
+                      a.lse ? a.lse + h * a.q.tokens + i : nullptr);
 }
 
 template <class T>

@@ -1,0 +1,75 @@
+"""The decoder operators at the ends of the numbers' range: weights, scales and
+values that are finite or infinite by the definition and must be so in the
+result, wherever in a sequence they stand.
+
+Helpers and the bounds of ordinary results are those of test_gpu_decoder."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+from test_gpu_decoder import DEV, TYPES, check_prompt, randn          # noqa: E402
+
+ALL = pytest.mark.parametrize("typ", ["f16", "bf16", "f32"])
+
+
+def scored(scores, typ, dim=32):
+    """Keys whose score with a query of one in the first place is `scores` (scale 1)."""
+    k = torch.zeros(len(scores), 1, dim, dtype=TYPES[typ][0], device=DEV)
+    k[:, 0, 0] = torch.as_tensor(scores).to(k)
+    return k
+
+
+def one_query(rows, typ, dim=32):
+    q = torch.zeros(rows, 1, dim, dtype=TYPES[typ][0], device=DEV)
+    q[:, :, 0] = 1.0
+    return q
+
+
+@pytest.mark.parametrize("rows", [1, 200])
+@pytest.mark.parametrize("work", [True, False])
+def test_prompt_large_values_float32(rows, work):
+    """Values of 1e35 whose largest weights come after smaller ones: the sum of 256 weights of at most 1 times 1e35
+    stays in float32's range."""
+    k = scored([0.0] * 64 + [4.8] * 256, "f32")
+    v = torch.full((320, 1, 32), 1e35, device=DEV)
+    v[::3] *= -1
+    check_prompt("f32", one_query(rows, "f32"), k, v, [rows], [320], 0, 1.0, work=work)
+    long = scored([0.0] * 1200 + [4.8] * 256, "f32")
+    v = torch.full((1456, 1, 32), 1e34, device=DEV)
+    check_prompt("f32", one_query(rows, "f32"), long, v, [rows], [1456], 0, 1.0, work=work)
+
+
+@pytest.mark.parametrize("n", [71, 1100])
+@pytest.mark.parametrize("rows", [1, 200])
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+def test_prompt_values_near_the_largest(typ, rows, n):
+    """Two keys count, the second ahead of the first by 1.3 (1.9 powers of two), both with values of 2e38."""
+    s = [-90.0] * n
+    s[0], s[70] = 0.0, 1.3
+    v = torch.full((n, 1, 32), 2e38, device=DEV).to(TYPES[typ][0])
+    check_prompt(typ, one_query(rows, typ), scored(s, typ), v, [rows], [n], 0, 1.0, work=False)
+
+
+@ALL
+def test_prompt_one_key_of_the_largest_value(typ):
+    dt = TYPES[typ][0]
+    big = torch.finfo(dt).max / (2 if typ == "f32" else 1)
+    v = torch.full((3, 2, 64), big, dtype=dt, device=DEV)
+    v[1] *= -1
+    q, k = randn((3, 2, 64), dt, 1), randn((3, 2, 64), dt, 2)
+    check_prompt(typ, q, k, v, [1, 1, 1], [1, 1, 1], 1)
+
+
+@pytest.mark.parametrize("n", [300, 1300])
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+def test_prompt_rows_beside_large_values(typ, n):
+    """Sums that leave float32's range before they are divided change no row that does not see their keys."""
+    dt = TYPES[typ][0]
+    q, k, v = randn((n, 2, 64), dt, 1), randn((n, 1, 64), dt, 2), randn((n, 1, 64), dt, 3)
+    ref = check_prompt(typ, q, k, v, [n], [n], 1, work=False)
+    v[n - 50:] = 3e38
+    out = check_prompt(typ, q, k, v, [n], [n], 1, work=False)
+    assert torch.equal(out[:n - 50], ref[:n - 50]) and torch.isfinite(out).all()
