@@ -174,7 +174,7 @@ __global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int 
     const int ex = __builtin_bit_cast(int, m) >> 23;              // biased exponent, 0 .. 255
     const int sh = ex == 0 || ex == 255 ? 0 : min(8 + 127 - ex, 126);
     float up = __builtin_bit_cast(float, (uint32_t)(127 + sh) << 23);
-    mul = fmaxf(__builtin_fabsf(scale) * kLog2e / up, 1e-30f);
+    mul = fmaxf(__builtin_fabsf(scale) * kLog2e / up, 1e-30f);    // not 0; scores of scaled queries are below 2^36
     up = scale < 0.f ? -up : up;
 #pragma unroll
     for (int g = 0; g < G; ++g) {

@@ -25,6 +25,10 @@ struct PromptArgs {
 // is below 2^-86).  2^28 keys then stay within the range.
 constexpr float kDown = 0x1p-40f, kUp = 0x1p40f;
 
+// What scores are multiplied by, never 0 (-infinity times 0 is a NaN, and hidden scores are that): for a scale of 0 the
+// least number, with which finite scores come to 2^-21 at most.
+__device__ __forceinline__ float multiplier(float scale) { return fmaxf(__builtin_fabsf(scale) * kLog2e, 0x1p-149f); }
+
 constexpr uint32_t kOutside = 0x80000000u;       // byte offset past every buffer: reads as 0
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *p) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, 0x7FFFFFFF, 0x00020000);

@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
 
   // queries, the sign of the scale folded in
   shortx8 qf[KS];
-  const float mul = fmaxf(__builtin_fabsf(a.scale) * kLog2e, 1e-30f);
+  const float mul = multiplier(a.scale);
   {
     const T *src = (const T *)a.q.data + (qa + min(r0 + l31, lq - 1)) * a.q.token_stride + head * a.q.head_stride;
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
 
   // Q: values 8 i + 4 half + e of query l31 (the order in which K's are read)
   float qf[DP / 2];
-  const float mul = fmaxf(__builtin_fabsf(a.scale) * kLog2e, 1e-30f), sign = a.scale < 0.f ? -1.f : 1.f;
+  const float mul = multiplier(a.scale), sign = a.scale < 0.f ? -1.f : 1.f;
   {
     const float *src = (const float *)a.q.data + (qa + min(r0 + l31, lq - 1)) * a.q.token_stride + head * a.q.head_stride;
 #pragma unroll

@@ -73,3 +73,14 @@ def test_prompt_rows_beside_large_values(typ, n):
     v[n - 50:] = 3e38
     out = check_prompt(typ, q, k, v, [n], [n], 1, work=False)
     assert torch.equal(out[:n - 50], ref[:n - 50]) and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-35, -1e-35, 1e-40])
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+def test_prompt_small_scales_of_large_scores(typ, scale):
+    """Products of queries and keys up to 1e37: a scale of 0 weighs every key alike, a small one as it says."""
+    dt, n = TYPES[typ][0], 200
+    size = {0.0: 1e17, 1e-35: 1e17, -1e-35: 1e17, 1e-40: 1e18}[scale]
+    q, k = randn((n, 2, 64), dt, 1, size), randn((n, 2, 64), dt, 2, size)
+    check_prompt(typ, q, k, randn((n, 2, 64), dt, 3), [n], [n], 1, scale)
+    check_prompt(typ, q, k, randn((n, 2, 64), dt, 3), [n], [n], 0, scale)
