@@ -13,6 +13,16 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxParts = 128;
 
+// x times a weight f that may have come to 0: an infinity or NaN that a row sees stays one, however little it weighs.
+__device__ __forceinline__ float weighed(float x, float f) { return __builtin_fabsf(x) < INFINITY || f != 0.f ? x * f : x; }
+
+// x f + y g, and the same, to the bit, where infinities and NaN have to be expected.
+__device__ __forceinline__ float joined(float x, float f, float y, float g) { return fmaf(x, f, y * g); }
+__device__ __forceinline__ float joined_odd(float x, float f, float y, float g) {
+  const bool finite = fmaxf(__builtin_fabsf(x), __builtin_fabsf(y)) < INFINITY && x == x && y == y;
+  return finite ? joined(x, f, y, g) : weighed(x, f) + weighed(y, g);
+}
+
 // One workgroup of 256 threads joins row `row` of `rows`: weights of the parts first (a thread each), then four values
 // a thread, the parts spread over the threads; every sum in a fixed order.  The first loads do not wait for the number
 // of parts that hold anything (count()); the others' values are left out.
@@ -58,7 +68,15 @@ __device__ __forceinline__ void join_parts(int64_t row, int64_t rows, int dim, i
     if (s0 != w) load(s0);
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      if (s0 + u * W < n) v += weight[s0 + u * W] * x[u];
+      if (s0 + u * W < n) {
+        const float f = weight[s0 + u * W];
+        if constexpr (kMeans) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] += weighed(x[u][e], f);
+        } else {
+          v += f * x[u];
+        }
+      }
   }
   sum[tid] = v;
   __syncthreads();

@@ -157,7 +157,8 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
   const floatx16 zero = {};
 
   // scores of a tile, transposed: keys 32 b + (r & 3) + 8 (r >> 2) + 4 half of query l31
-  auto scores = [&](const unsigned char *sk, floatx16 *s) {
+  auto scores = [&](const unsigned char *sk, floatx16 *s, int lane) {
+    const int half = lane >> 5, l31 = lane & 31;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       s[b] = zero;
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
       }
     }
   };
-  auto hide = [&](int t, floatx16 *s) {
+  auto hide = [&](int t, floatx16 *s, int half, int lim) {
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -185,8 +186,8 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     return mx;
   };
   // follow the rows' maxima where they have grown, each row by its own scores alone, so that no row's result depends on
-  // another's
-  auto follow = [&](float mx) {
+  // another's; in the walk with care o may hold infinities and NaN
+  auto follow = [&](float mx, auto care) {
     mx *= mul;
     if (__any(mx > m + (kTop<T> + 2.f))) {
       const float rm = fmaxf(mx, other_half(mx)), mn = rm > m + (kTop<T> + 2.f) ? rm - kTop<T> : m;
@@ -194,7 +195,14 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
       m = mn;
       l *= f;
 #pragma unroll
-      for (int i = 0; i < DB; ++i) o[i] *= f;
+      for (int i = 0; i < DB; ++i) {
+        if constexpr (decltype(care)::value) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[i][r] = weighed(o[i][r], f);
+        } else {
+          o[i] *= f;
+        }
+      }
     }
   };
   auto weights = [&](const floatx16 *s, shortx8 *pf, float by) {
@@ -208,7 +216,8 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
         pf[2 * b + (r >> 3)][r & 7] = __builtin_bit_cast(short, (T)(e * by));  // p as the inputs' type: 2^-9 (2^-12) each
       }
   };
-  auto values = [&](const unsigned char *sv, int i, int ks) {
+  auto values = [&](const unsigned char *sv, int i, int ks, int lane) {
+    const int half = lane >> 5, l15 = lane & 15;
     const int r = 16 * ks + 4 * half + (l15 >> 2), c = 4 * i + 2 * (lane >> 4 & 1) + ((l15 & 3) >> 1);
     const unsigned char *p = sv + r * (CH * 16) + (c ^ swz_v<DP>(r)) * 16 + 8 * (l15 & 1);
     const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)p);
@@ -257,7 +266,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     // past the last tile that a row of this wave sees there is nothing to do but to load and to wait
     const int end = min(tiles, (lim_hi + kBN) / kBN);
     // tile k of this group, whose scores are s; leaves those of the next in sn
-    auto step = [&](int k, floatx16 *s, floatx16 *sn) {
+    auto step = [&](int k, floatx16 *s, floatx16 *sn) __attribute__((always_inline)) {
       const int t = first + k * KG, next = t + KG;
       arrived();
       if (next < tiles) issue_v(next, (k + 1) & 1);
@@ -293,10 +302,10 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
       }
       if (next < end) {
         if (masked(next)) {
-          hide(next, sn);
+          hide(next, sn, half, lim);
           mx = largest(sn);
         }
-        follow(mx);
+        follow(mx, std::false_type{});
       }
     };
     floatx16 s[2], sn[2];
@@ -305,17 +314,20 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     if (first < tiles) issue_v(first, 0);
     if (first + KG < tiles) issue_k(first + KG, 1);
     if (first < end) {
-      scores(lds[0][0], s);
-      if (masked(first)) hide(first, s);
-      follow(largest(s));
+      scores(lds[0][0], s, lane);
+      if (masked(first)) hide(first, s, half, lim);
+      follow(largest(s), std::false_type{});
     }
     for (int k = 0; t0 + k * KG < tiles; k += 2) {
       step(k, s, sn);
       if (t0 + (k + 1) * KG < tiles) step(k + 1, sn, s);
     }
   }
+  // From here on the lane's place is worked out anew: the walk is short of registers.
+  const int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), lnh = ln >> 5;
+  const int lim2 = max(last_key(r0 + (ln & 31)), -1);
   // whether any wave of the workgroup found a number that is not finite
-  auto odd = [&] {
+  auto odd = [&]() __attribute__((always_inline)) {
     int x = 0;
 #pragma unroll
     for (int i = 0; i < DB; ++i)
@@ -324,18 +336,19 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     int *found = (int *)stage;
     __syncthreads();                                         // the tiles are done with
     x = __any(x);
-    if (lane == 0) found[threadIdx.x >> 6] = x;
+    if (ln == 0) found[group * 4 + wave] = x;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 4 * KG; ++w) x |= found[w];
     return __builtin_amdgcn_readfirstlane(x);
   };
-  // Again, with care: infinities and NaN among the values of a tile that not every row sees whole are kept out of the
-  // product (0 times one of them is a NaN) and reach the rows that see them by counts.  And once more if a sum has left
-  // float32's range (f16 values stay far below).  (As a loop over both the kernel for heads of 128 spills registers.)
+  // Again, with care: infinities and NaN among the values are kept out of the product (0 times one of them is a NaN, and
+  // a weight may come to 0 as well as be hidden) and reach the rows that see them by counts.  And once more if a sum has
+  // left float32's range (f16 values stay far below).  (As a loop over both the kernel for heads of 128 spills registers.)
   float up = 1.f;
-  if (odd()) {
-    auto careful = [&](float by) {
+  const bool again = odd();
+  if (again) {
+    auto careful = [&](float by) __attribute__((always_inline)) {
       clear();
       for (int k = 0; t0 + k * KG < tiles; ++k) {
         const int t = t0 + k * KG + group;
@@ -348,40 +361,35 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
         if (t >= tiles || t * kBN > lim_hi) continue;
         floatx16 s[2];
         shortx8 pf[4];
-        scores(lds[0][0], s);
-        hide(t, s);
-        follow(largest(s));
+        scores(lds[0][0], s, ln);
+        hide(t, s, lnh, lim2);
+        follow(largest(s), std::true_type{});
         weights(s, pf, by);
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
-          floatx16 nan = zero, up = zero, down = zero;
+          floatx16 above = zero, below = zero;               // infinities of both signs (a NaN is both) that a row sees
 #pragma unroll
           for (int ks = 0; ks < 4; ++ks) {
-            shortx8 vf = values(lds[0][1], i, ks);
-            if (masked(t)) {
-              constexpr int inf = std::is_same_v<T, _Float16> ? 0x7C00 : 0x7F80;
-              const short one = __builtin_bit_cast(short, (T)1.f);
-              shortx8 vn, vu, vd, seen;
+            shortx8 vf = values(lds[0][1], i, ks, ln);
+            constexpr int inf = std::is_same_v<T, _Float16> ? 0x7C00 : 0x7F80;
+            const short one = __builtin_bit_cast(short, (T)1.f);
+            shortx8 va, vb, seen;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int mag = vf[e] & 0x7FFF;
-                vn[e] = mag > inf ? one : 0;
-                vu[e] = vf[e] == inf ? one : 0;
-                vd[e] = mag == inf && vf[e] < 0 ? one : 0;
-                if (mag >= inf) vf[e] = 0;
-                seen[e] = t * kBN + 16 * ks + 4 * half + (e & 3) + 8 * (e >> 2) <= lim ? one : 0;
-              }
-              nan = mfma<T>(vn, seen, nan);
-              up = mfma<T>(vu, seen, up);
-              down = mfma<T>(vd, seen, down);
+            for (int e = 0; e < 8; ++e) {
+              const int mag = vf[e] & 0x7FFF;
+              va[e] = mag > inf || vf[e] == inf ? one : 0;
+              vb[e] = mag > inf || (mag == inf && vf[e] < 0) ? one : 0;
+              if (mag >= inf) vf[e] = 0;
+              seen[e] = t * kBN + 16 * ks + 4 * lnh + (e & 3) + 8 * (e >> 2) <= lim2 ? one : 0;
             }
+            above = mfma<T>(va, seen, above);
+            below = mfma<T>(vb, seen, below);
             o[i] = mfma<T>(vf, pf[ks], o[i]);
           }
-          if (masked(t)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-              o[i][r] += nan[r] > 0.f || (up[r] > 0.f && down[r] > 0.f) ? NAN
-                         : up[r] > 0.f ? INFINITY : down[r] > 0.f ? -INFINITY : 0.f;
+          for (int r = 0; r < 16; ++r) {
+            if (above[r] > 0.f) o[i][r] += INFINITY;
+            if (below[r] > 0.f) o[i][r] -= INFINITY;
           }
         }
       }
@@ -399,7 +407,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
   if constexpr (KG > 1) {                                    // the second group's rows go through LDS to the first
     static_assert(KG == 2 && sizeof(stage) >= (4 * DB * 16 * 64 + 512) * 4, "one other group");
     __syncthreads();                                         // the tiles are done with
-    float *oo = (float *)stage + wave * (DB * 16 * 64) + lane, *ml = (float *)stage + 4 * DB * 16 * 64 + tid;
+    float *oo = (float *)stage + wave * (DB * 16 * 64) + ln, *ml = (float *)stage + 4 * DB * 16 * 64 + wave * 64 + ln;
     if (group == 1) {
       ml[0] = m;
       ml[256] = l;
@@ -417,10 +425,17 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     const float inv = l == 0.f ? 0.f : 1.f / l;
     f0 *= inv;
     f1 *= inv;
+    if (again) {
 #pragma unroll
-    for (int i = 0; i < DB; ++i)
+      for (int i = 0; i < DB; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[i][r] = (o[i][r] * f0 + oo[(i * 16 + r) * 64] * f1) * up;
+        for (int r = 0; r < 16; ++r) o[i][r] = joined_odd(o[i][r], f0, oo[(i * 16 + r) * 64], f1) * up;
+    } else {
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = joined(o[i][r], f0, oo[(i * 16 + r) * 64], f1);
+    }
   } else {
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -428,7 +443,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * inv * up;
   }
-  const int row = r0 + l31;
+  const int row = r0 + (ln & 31);
   if (row >= lq) return;
   if (a.part) {
     const int64_t x = (qa + row) * a.heads + head;
@@ -437,10 +452,10 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     for (int i = 0; i < DB; ++i)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4)
-        if (32 * i + 8 * r4 + 4 * half < a.dim)
-          *(floatx4 *)(dst + 32 * i + 8 * r4 + 4 * half) =
+        if (32 * i + 8 * r4 + 4 * lnh < a.dim)
+          *(floatx4 *)(dst + 32 * i + 8 * r4 + 4 * lnh) =
               floatx4{o[i][4 * r4], o[i][4 * r4 + 1], o[i][4 * r4 + 2], o[i][4 * r4 + 3]};
-    if (half == 0) {
+    if (lnh == 0) {
       float *ml = a.part + (int64_t)a.q.tokens * a.heads * gridDim.z * a.dim + (x * gridDim.z + split) * 2;
       ml[0] = m;
       ml[1] = l;
@@ -452,7 +467,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
   for (int i = 0; i < DB; ++i)
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) {
-      const int d = 32 * i + 8 * r4 + 4 * half;
+      const int d = 32 * i + 8 * r4 + 4 * lnh;
       if (d < a.dim) {
         struct alignas(8) { T v[4]; } w;
 #pragma unroll
@@ -460,7 +475,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
         *(decltype(w) *)(dst + d) = w;
       }
     }
-  if (a.lse && half == 0) a.lse[(int64_t)head * a.q.tokens + qa + row] = (m + __builtin_log2f(l)) * kLn2;
+  if (a.lse && lnh == 0) a.lse[(int64_t)head * a.q.tokens + qa + row] = (m + __builtin_log2f(l)) * kLn2;
 }
 
 // The rows' parts: a workgroup per row.  Rows of no sequence are passed over.

@@ -158,7 +158,14 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
         m = mn;
         l *= f;
 #pragma unroll
-        for (int i = 0; i < DB; ++i) o[i] *= f;
+        for (int i = 0; i < DB; ++i) {
+          if constexpr (kAgain) {                            // o may hold infinities and NaN
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[i][r] = weighed(o[i][r], f);
+          } else {
+            o[i] *= f;
+          }
+        }
       }
       const float mu = m == -INFINITY ? 0.f : m;
       auto weight = [&](int r) {
@@ -210,7 +217,8 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
 #pragma unroll
     for (int r = 0; r < 16; ++r) odd |= !(__builtin_fabsf(o[i][r]) < INFINITY);
   float up = 1.f;
-  if (__syncthreads_or(odd)) {                               // a sum has left float32's range
+  const bool again = __builtin_amdgcn_readfirstlane(__syncthreads_or(odd));
+  if (again) {                                               // rows see an infinity or NaN, or a sum has left float32's range
     walk(std::true_type{});
     up = kUp;
   }
@@ -237,8 +245,13 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
       }
       __syncthreads();
       if (group == 0) {
+        if (again) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[i][r] = (o[i][r] * f0 + other_o[tid][r] * f1) * up;
+          for (int r = 0; r < 16; ++r) o[i][r] = joined_odd(o[i][r], f0, other_o[tid][r], f1) * up;
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[i][r] = joined(o[i][r], f0, other_o[tid][r], f1);
+        }
       }
       __syncthreads();
     }

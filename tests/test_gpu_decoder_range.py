@@ -84,3 +84,26 @@ def test_prompt_small_scales_of_large_scores(typ, scale):
     q, k = randn((n, 2, 64), dt, 1, size), randn((n, 2, 64), dt, 2, size)
     check_prompt(typ, q, k, randn((n, 2, 64), dt, 3), [n], [n], 1, scale)
     check_prompt(typ, q, k, randn((n, 2, 64), dt, 3), [n], [n], 0, scale)
+
+
+@ALL
+@pytest.mark.parametrize("rows,n,work", [(300, 300, False), (1300, 1300, False), (3, 1300, True), (3, 1300, False),
+                                         (70, 6000, True)])
+@pytest.mark.parametrize("lead", [0.0, 60.0, 120.0])
+def test_prompt_seen_infinities(typ, rows, n, work, lead):
+    """An infinite value that a row sees is infinite in its result, however little its key weighs and wherever the key
+    lies: in tiles that every row sees or not, before keys far ahead of it or after."""
+    s = [0.0] * n
+    first = n - rows + 1                          # keys that every row sees
+    where = [5, 70, 140, n // 2, n - 2]
+    for i in where:
+        s[i] = -lead
+    s[first // 2] = lead                          # far ahead of all
+    v = randn((n, 1, 32), TYPES[typ][0], 3)
+    for d, i in enumerate(where):
+        v[i, 0, d] = math.inf if d % 2 else -math.inf
+        v[i, 0, 8] = math.inf
+        v[i, 0, 9] = math.inf if d < 3 else -math.inf
+        v[i, 0, 10 + d] = math.nan
+    check_prompt(typ, one_query(rows, typ), scored(s, typ), v, [rows], [n], 1, 1.0, work=work)
+    check_prompt(typ, one_query(rows, typ), scored(s, typ), v, [rows], [n], 0, 1.0, work=work)
