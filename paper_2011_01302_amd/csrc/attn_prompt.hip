@@ -437,7 +437,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
         for (int r = 0; r < 16; ++r) o[i][r] = joined(o[i][r], f0, oo[(i * 16 + r) * 64], f1);
     }
   } else {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f && m == -INFINITY ? 0.f : 1.f / l;   // no key seen (m is +infinity where scores overflow)
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll

@@ -10,7 +10,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
-from test_gpu_decoder import DEV, TYPES, check_prompt, randn          # noqa: E402
+from test_gpu_decoder import DEV, TYPES, check_prompt, prompt, randn          # noqa: E402
 
 ALL = pytest.mark.parametrize("typ", ["f16", "bf16", "f32"])
 
@@ -107,3 +107,14 @@ def test_prompt_seen_infinities(typ, rows, n, work, lead):
         v[i, 0, 10 + d] = math.nan
     check_prompt(typ, one_query(rows, typ), scored(s, typ), v, [rows], [n], 1, 1.0, work=work)
     check_prompt(typ, one_query(rows, typ), scored(s, typ), v, [rows], [n], 0, 1.0, work=work)
+
+
+@pytest.mark.parametrize("n,work", [(200, False), (1300, False), (3000, True)])
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+def test_prompt_scores_beyond_float32_are_not_zeros(typ, n, work):
+    """Where scores times log2(e) leave float32's range there is no result; it reads as NaN, not as a row of zeros."""
+    dt = TYPES[typ][0]
+    q, k = (torch.full((3 if x else n, 1, 32), 2.5e18, dtype=dt, device=DEV) for x in (1, 0))   # scores of 3e38
+    k[1::2] *= 0.5
+    out, lse, _ = prompt(typ, q, k, randn((n, 1, 32), dt, 3), [3], [n], 0, 1.5, work)
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
