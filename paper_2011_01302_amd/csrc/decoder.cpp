@@ -280,9 +280,13 @@ extern "C" int ios_cache_status(const ios_cache *c, void *hip_stream, int32_t *f
     need(flags != nullptr, IOS_E_ARG, "null flags");
     hipStream_t s = (hipStream_t)hip_stream;
     int32_t f = 0;
-    hip_check(hipMemcpyAsync(&f, (int32_t *)c->work + CW_FLAGS, sizeof(f), hipMemcpyDeviceToHost, s), "hipMemcpyAsync");
+    int32_t *word = (int32_t *)c->work + CW_FLAGS;
+    hip_check(hipMemcpyAsync(&f, word, sizeof(f), hipMemcpyDeviceToHost, s), "hipMemcpyAsync");
     hip_check(hipStreamSynchronize(s), "hipStreamSynchronize");
-    if (f) hip_check(hipMemset((int32_t *)c->work + CW_FLAGS, 0, sizeof(f)), "hipMemset(flags)");
+    if (f) {                                                 // on the caller's stream: before whatever is called next
+      hip_check(hipMemsetAsync(word, 0, sizeof(f), s), "hipMemsetAsync(flags)");
+      hip_check(hipStreamSynchronize(s), "hipStreamSynchronize");
+    }
     *flags = f;
   });
 }

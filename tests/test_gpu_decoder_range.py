@@ -10,7 +10,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
-from test_gpu_decoder import DEV, TYPES, check_prompt, prompt, randn          # noqa: E402
+from test_gpu_decoder import DEV, TYPES, Cache, I, check_prompt, i32, prompt, randn          # noqa: E402
 
 ALL = pytest.mark.parametrize("typ", ["f16", "bf16", "f32"])
 
@@ -118,3 +118,25 @@ def test_prompt_scores_beyond_float32_are_not_zeros(typ, n, work):
     k[1::2] *= 0.5
     out, lse, _ = prompt(typ, q, k, randn((n, 1, 32), dt, 3), [3], [n], 0, 1.5, work)
     assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+def test_status_stays_on_its_stream():
+    """The flags are cleared on the caller's stream, so before whatever it is given next, and without waiting for the
+    default stream: that is still at work when the calls return."""
+    c = Cache(1, 32, 32, 2, 2, 4)
+    seq, add = i32([0]), i32([100])               # more than there are pages for
+    mine = torch.cuda.Stream()
+    a = torch.zeros(8192, 8192, dtype=torch.bfloat16, device=DEV)
+    b = torch.empty_like(a)
+    torch.mm(a, a, out=b)
+    torch.cuda.synchronize()
+    seen = []
+    for _ in range(200):                          # about 1 ms each
+        torch.mm(a, a, out=b)
+    for _ in range(3):
+        I.ios_cache_reserve(c.c, 1, seq.data_ptr(), add.data_ptr(), mine.cuda_stream)
+        seen += [I.ios_cache_status(c.c, mine.cuda_stream), I.ios_cache_status(c.c, mine.cuda_stream)]
+    busy = not torch.cuda.default_stream().query()
+    torch.cuda.synchronize()
+    assert seen == [I.IOS_CACHE_NO_PAGES, 0] * 3
+    assert busy
