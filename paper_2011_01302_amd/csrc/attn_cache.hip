@@ -216,11 +216,8 @@ __global__ __launch_bounds__(kThreadsA) void attn_cache_kernel(CacheView c, int 
       issue(k + kStages - 1, next);
       next = page_of(k + kStages);
       wait_loads<NL *(kStages - 1)>();
-    } else if (kStages > 3 && ahead == 2) {
-      wait_loads<NL * 2>();
-    } else if (kStages > 2 && ahead == 1) {
-      wait_loads<NL>();
     } else {
+      static_assert(kStages == 2, "a longer ring has other tiles on their way behind this one");
       wait_loads<0>();
     }
     if (!(sound >> ahead & 1)) continue;
