@@ -1,9 +1,11 @@
 // Joining the parts of attention rows whose keys were spread over workgroups.
 //
-// Part s of a row leaves in the workspace sum_j p_j v_j ([row][part][dim] floats), or that divided by sum_j p_j (`kMeans`:
-// values may reach to float32's largest, and sums of them not), and behind all of those its reference m and the sum of
+// Part s of a row leaves in the workspace sum_j p_j v_j ([row][part][dim] floats), or half of that divided by sum_j p_j
+// (`kMeans`: values may reach to float32's largest, and sums of them not), and behind all of those its reference m and the sum of
 // p_j = 2^(score_j - m) ([row][part][2]).
 #pragma once
+
+#include <type_traits>
 
 #include "decoder.h"
 
@@ -21,6 +23,17 @@ __device__ __forceinline__ float joined(float x, float f, float y, float g) { re
 __device__ __forceinline__ float joined_odd(float x, float f, float y, float g) {
   const bool finite = fmaxf(__builtin_fabsf(x), __builtin_fabsf(y)) < INFINITY && x == x && y == y;
   return finite ? joined(x, f, y, g) : weighed(x, f) + weighed(y, g);
+}
+
+// Of half a mean of T's values, the mean.  It is never beyond T's largest number: where rounded weights say so, it is that.
+template <class T>
+__device__ __forceinline__ T doubled(float half) {
+  constexpr float most = std::is_same_v<T, _Float16> ? 65504.f : std::is_same_v<T, float> ? 0x1.fffffep127f : 0x1.fep127f;
+  return (T)(2.f * (__builtin_fabsf(half) > 0.5f * most ? __builtin_copysignf(0.5f * most, half) : half));
+}
+template <class T>
+__device__ __forceinline__ T doubled_odd(float half) {
+  return __builtin_fabsf(half) < INFINITY ? doubled<T>(half) : (T)half;
 }
 
 // One workgroup of 256 threads joins row `row` of `rows`: weights of the parts first (a thread each), then four values
@@ -84,7 +97,10 @@ __device__ __forceinline__ void join_parts(int64_t row, int64_t rows, int dim, i
     for (int y = 1; y < W; ++y) v += sum[tid + y * Q];
     struct alignas(4 * sizeof(T)) { T v[4]; } r;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r.v[e] = (T)(kMeans ? v[e] : ll == 0.f ? 0.f : v[e] / ll);
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (kMeans) r.v[e] = doubled_odd<T>(v[e]);
+      else r.v[e] = (T)(ll == 0.f ? 0.f : v[e] / ll);
+    }
     *(decltype(r) *)(out + 4 * tid) = r;
   }
   if (lse && tid == 0) *lse = (mm + __builtin_log2f(ll)) * kLn2;

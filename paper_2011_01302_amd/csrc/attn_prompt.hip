@@ -422,7 +422,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(m1 - mu);
     m = mm;
     l = l * f0 + ml[256] * f1;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : 0.5f / l;               // half means: they stay below float32's largest
     f0 *= inv;
     f1 *= inv;
     if (again) {
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
         for (int r = 0; r < 16; ++r) o[i][r] = joined(o[i][r], f0, oo[(i * 16 + r) * 64], f1);
     }
   } else {
-    const float inv = l == 0.f && m == -INFINITY ? 0.f : 1.f / l;   // no key seen (m is +infinity where scores overflow)
+    const float inv = l == 0.f && m == -INFINITY ? 0.f : 0.5f / l;  // no key seen (m is +infinity where scores overflow)
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll
@@ -463,18 +463,22 @@ __global__ __launch_bounds__(256 * KG, 2) void attn_prompt_kernel(PromptArgs a) 
     return;
   }
   T *dst = (T *)a.out.data + (qa + row) * a.out.token_stride + head * a.out.head_stride;
+  auto store = [&](auto number) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < DB; ++i)
+    for (int i = 0; i < DB; ++i)
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const int d = 32 * i + 8 * r4 + 4 * lnh;
-      if (d < a.dim) {
-        struct alignas(8) { T v[4]; } w;
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int d = 32 * i + 8 * r4 + 4 * lnh;
+        if (d < a.dim) {
+          struct alignas(8) { T v[4]; } w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w.v[e] = (T)o[i][4 * r4 + e];
-        *(decltype(w) *)(dst + d) = w;
+          for (int e = 0; e < 4; ++e) w.v[e] = number(o[i][4 * r4 + e]);
+          *(decltype(w) *)(dst + d) = w;
+        }
       }
-    }
+  };
+  if (again) store([](float x) { return doubled_odd<T>(x); });
+  else store([](float x) { return doubled<T>(x); });
   if (a.lse && lnh == 0) a.lse[(int64_t)head * a.q.tokens + qa + row] = (m + __builtin_log2f(l)) * kLn2;
 }
 

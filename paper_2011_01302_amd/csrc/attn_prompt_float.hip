@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
     float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(m1 - mu);
     m = mm;
     l = l * f0 + other_ml[tid][1] * f1;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : 0.5f / l;             // half means: they stay below float32's largest
     f0 *= inv;
     f1 *= inv;
 #pragma unroll
@@ -283,7 +283,10 @@ __global__ __launch_bounds__(kGroupThreads * KG, 2) void attn_prompt_float_kerne
     for (int r4 = 0; r4 < 4; ++r4) {
       const int d = 32 * i + 8 * r4 + 4 * half;
       if (d < a.dim) {
-        *(floatx4 *)(dst + d) = floatx4{o[i][4 * r4], o[i][4 * r4 + 1], o[i][4 * r4 + 2], o[i][4 * r4 + 3]};
+        floatx4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = doubled_odd<float>(o[i][4 * r4 + e]);
+        *(floatx4 *)(dst + d) = w;
       }
     }
   if (a.lse && half == 0) a.lse[(int64_t)head * a.q.tokens + qa + row] = (m + __builtin_log2f(l)) * kLn2;

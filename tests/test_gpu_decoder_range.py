@@ -140,3 +140,33 @@ def test_status_stays_on_its_stream():
     torch.cuda.synchronize()
     assert seen == [I.IOS_CACHE_NO_PAGES, 0] * 3
     assert busy
+
+
+@ALL
+@pytest.mark.parametrize("rows,n,work", [(1, 7, False), (200, 200, False), (300, 1300, False), (40, 3000, True)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_prompt_values_of_the_largest_number(typ, rows, n, work, dim):
+    """A mean of the type's largest number is that number, not infinity, whatever the weights' rounding."""
+    dt = TYPES[typ][0]
+    q, k = randn((rows, 2, dim), dt, 1), randn((n, 1, dim), dt, 2)
+    big = torch.finfo(dt).max
+    v = torch.full((n, 1, dim), big, dtype=dt, device=DEV)
+    v[:, :, 1::2] *= -1
+    v[n // 2:, 0, 5] = math.inf                    # which some rows see
+    out, _, _ = prompt(typ, q, k, v, [rows], [n], 1, None, work)
+    out, u = out.double().cpu(), TYPES[typ][2]
+    seen = torch.arange(rows) + n - rows >= n // 2
+    assert (out[seen][:, :, 5] == math.inf).all()
+    out[:, :, 5] = -big
+    out[:, :, 1::2] *= -1
+    assert torch.isfinite(out).all() and (out >= big * (1 - 4 * u - 2.0 ** -20)).all() and (out <= big).all()
+
+
+@pytest.mark.parametrize("n,work", [(2000, False), (900, False), (6000, True)])
+@pytest.mark.parametrize("typ,step", [("f16", 2.0 ** -11), ("bf16", 2.0 ** -8)])
+def test_prompt_weights_that_all_round_up(typ, step, n, work):
+    """Weights half a unit of the type above that of the first keys, all rounded up, their sum not."""
+    big = torch.finfo(TYPES[typ][0]).max
+    v = torch.full((n, 1, 32), big, dtype=TYPES[typ][0], device=DEV)
+    out, _, _ = prompt(typ, one_query(1, typ), scored([0.0] * 128 + [step] * (n - 128), typ), v, [1], [n], 0, 1.0, work)
+    assert (out == big).all()
