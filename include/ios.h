@@ -398,7 +398,11 @@ typedef struct {
 
 /* An attention: o_i = sum_j softmax_j(scale q_i . k_j) v_j, for `heads` heads
  * of queries, of which heads / kv_heads read each head of keys and values.
- * A row that sees no key gives 0 (and -infinity as its log-sum-exp). */
+ * A row that sees no key gives 0 (and -infinity as its log-sum-exp).  Finite
+ * values give finite results; an infinity that a row sees is one in its result,
+ * however little its key weighs.  A row with a NaN or +infinity among its scores
+ * is NaN, also where a score times log2(e) passes float32's largest; one that
+ * passes the lowest weighs nothing. */
 typedef struct {
   int32_t dtype;             /* IOS_F32 / F16 / BF16, of every tensor of the call      */
   int32_t heads, kv_heads;   /* heads % kv_heads == 0                                  */
@@ -429,7 +433,7 @@ int ios_attn_work_bytes(const ios_attn_desc *d, int64_t q_tokens, int64_t *bytes
  * Errors: IOS_E_ARG (null pointer, type, sizes, misaligned tensor, workspace
  * below ios_attn_work_bytes), IOS_E_SHAPE (heads % kv_heads, k and v of
  * different lengths, q and out of different lengths), IOS_E_UNSUPPORTED
- * (head_dim), IOS_E_HIP. */
+ * (head_dim, too many queries and heads), IOS_E_HIP. */
 int ios_attn_prompt(const ios_attn_desc *d, const ios_tokens *q, const ios_tokens *k, const ios_tokens *v,
                     const ios_tokens *out, float *lse, const int32_t *cu_q, const int32_t *cu_k, void *work,
                     int64_t work_bytes, void *hip_stream);
@@ -522,8 +526,8 @@ int ios_cache_compact(const ios_cache *c, int32_t *live, void *hip_stream);
 int ios_cache_copy(const ios_cache *c, int32_t n, const int32_t *src, const int32_t *dst, void *hip_stream);
 
 /* Wait for `hip_stream`, read what the calls above could not report, and clear
- * it: bit 0 = ios_cache_reserve ran out of pages, bit 1 = of table entries,
- * bit 2 = ios_cache_fork met a child in use.
+ * it on the same stream: bit 0 = ios_cache_reserve ran out of pages, bit 1 = of
+ * table entries, bit 2 = ios_cache_fork met a child in use.
  * Errors: IOS_E_ARG, IOS_E_HIP. */
 int ios_cache_status(const ios_cache *c, void *hip_stream, int32_t *flags);
 

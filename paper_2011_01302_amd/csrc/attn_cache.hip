@@ -8,15 +8,18 @@
 // joined at the end, the ranges in a second launch.
 //
 // 32 sequences of 8192 .. 32031 tokens, 8 heads of 128, 4 queries each: 823 MB in
-// 175 us, 4.7 TB/s (a large copy moves 4.95); the loads alone take 152 us.  One
-// sequence of 131072 tokens and 2 such heads: 14 us, and 4 for the join.  Tiles
+// 176 us, 4.7 TB/s (a large copy moves 4.95), and 5 for the join; the loads alone
+// take 152 us.  Results in f16 take 239 us, in float32 382 (more products, and
+// codes converted one by one).  One sequence of 131072 tokens and 2 such heads:
+// 14 us, and 4 for the join.  Tiles
 // reach LDS through a ring of direct copies per wave, two tiles deep: with
 // 16 waves a CU about 80 KB are on their way, and no barrier is needed before
 // the end (registers and no ring: 595 us; four waves and three tiles: 220).
 //
-// Scores are exact up to 32-bit sums: with q summed over the values of a
-// group, s . (z + s_k c) = z sum(q) + s_k (c . q), c exact in f16 and q too
-// (bf16 after scaling a row by a power of two; float32 as two f16 parts).
+// Scores: with q summed over the values of a group, q . (z + s c) = z sum(q) +
+// s (c . q), c exact in f16 and q too (bf16 after scaling a row by a power of two;
+// float32 as two f16 parts, 22 bits).  sum(q) meets z in two f16 parts as well
+// (22 bits, where one product takes all groups); the rest is summed in 32 bits.
 // The second product for bf16 results rounds p and the values z + s c to f16
 // (2^-12 each, against 2^-9 of the result).  For f16 and float32 that would
 // show in the result, so there the codes stay exact and p s is split into two
@@ -38,10 +41,12 @@ typedef __bf16 bfx8 __attribute__((ext_vector_type(8)));
 constexpr int kCols = 16;                // queries (heads of one key head) of a workgroup
 constexpr int kWavesA = 8, kThreadsA = 64 * kWavesA;
 constexpr int kStages = 2;               // tiles of a wave's ring
-// Parts of a sequence's keys: kWantBlocks workgroups if they fill the chip's 256 CUs twice over (they end at
-// different times: 32 sequences of 8k .. 32k keys took 187 us in parts for 512 workgroups, 180 for 1024, 191 for 2048),
-// at least kMinKeys keys each (a tile for every wave), at most kMaxSplits (131072 keys in 512 parts and their join took
-// 27 us, 20 in 256, 18 in 128), and none (no second launch) below kOneKeys: 785 keys take 11 us in one part, 13 in 3.
+// Parts of a sequence's keys (bf16; us of both sides): kWantBlocks workgroups, twice what the chip holds at once, as they
+// end at different times (for 512, 1024 and 2048: 32 sequences of 8k .. 32k keys 195, 188, 193; 16 of 16000 71, 70, 73; but
+// 16 of 5000 27, 30, 38 and 4 of 16000 17, 21, 21); at least kMinKeys keys each, a tile for every wave (for 128, 256 and 512:
+// one sequence of 5000 9.9, 10.4, 11.8; 4 of 1300 9.2, 9.7, 12.0; 16 of 1300 21, 18, 15); at most kMaxSplits (131072 keys in
+// 64 parts and their join 22.7, in 128 18.4); and none, so no second launch, below kOneKeys (in one part and in several: 600
+// keys 8.5 and 10.1, 785 9.9 and 10.0, 1000 11.2 and 10.1, 1300 12.8 and 10.1; 16 sequences of 785 10.6 and 13.9).
 constexpr int kMaxSplits = kMaxParts, kWantBlocks = 1024, kMinKeys = 256, kOneKeys = 1024;
 typedef __attribute__((address_space(3))) void lds_void;
 // one tile in the ring, whole 1024-byte loads

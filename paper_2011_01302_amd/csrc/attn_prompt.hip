@@ -9,12 +9,12 @@
 // product's operand as they stand (keys 8 i + 4 h + 0 .. 3 of a tile lie in
 // half h; V is read in that order).
 //
-// Bound by the matrix rate and the power behind it for heads of 96 and 128
-// (16384 causal tokens, 32 heads of 128: 2.03 ms, 1080 TFLOP/s, where a large
-// matrix product of the library reaches 1130), by the exponentials and the
-// other vector instructions of the softmax for smaller heads (4096 causal
-// tokens, 16 heads of 64: 60 us, 570 TFLOP/s), by its longest rows where
-// prompts of different lengths are packed.
+// Bound by power for heads of 96 and 128 (16384 causal tokens, 32 heads of 128:
+// 1.97 ms, 1120 TFLOP/s at 1.73 GHz, matrix cores 56 and vector units 51 per
+// cent busy; a large matrix product of the library reaches 1130 .. 1220 at 1.72),
+// by the exponentials and the other vector instructions of the softmax for
+// smaller heads (4096 causal tokens, 16 heads of 64: 61 us, 560 TFLOP/s), by its
+// longest rows where prompts of different lengths are packed.
 #include <type_traits>
 
 #include "attn_prompt.h"
@@ -34,10 +34,10 @@ typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
 constexpr int kBM = kRows, kBN = kKeys;
 // Fewer than kFewBlocks workgroups: the keys of a row are spread over workgroups (a second launch joins them), in parts
-// of at least kPartKeys keys (32 heads of 128: 1 row over 6000 keys 18 us, 96 in one part).  Up to kTwoGroups
-// workgroups, and from kTwoKeys keys on: over two groups of waves of one workgroup (2048 causal tokens, 16 heads of 64,
-// 272 workgroups: 26.6 us, 30.5 with one group; 32 heads of 128, 544 workgroups: 57.5 and 53.3; 512 tokens, 160
-// workgroups: 17.5 and 16.7).
+// of at least kPartKeys keys (32 heads of 128 over 6000 keys: 256 rows, 96 workgroups, 65 us, 90 in one part; 512 rows,
+// 160 workgroups, 105 and 92; 1 row 18.8 us).  Up to kTwoGroups workgroups, and from kTwoKeys keys on: over two groups of
+// waves of one workgroup (16 heads of 64, 2048 causal tokens, 272 workgroups: 27.5 us, 32.3 with one group; 32 heads of
+// 128, 288 workgroups: 27.7 and 28.6, 416: 40.2 and 41.2, 544: 58.1 and 54.3).
 constexpr int kFewBlocks = 129, kPartKeys = 256, kTwoGroups = 320, kTwoKeys = 1024;
 // p = 2^(score - m), m kTop below the row's largest score when it was last followed, which it is when a score passes it
 // by kTop + 2 (sums are in 32 bits).  f16 then holds p from 2^15 down to 2^-38 of the largest.

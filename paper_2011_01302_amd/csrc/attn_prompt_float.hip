@@ -2,8 +2,9 @@
 // attn_prompt.hip on v_mfma_f32_32x32x2_f32, every number in 32 bits.  Bound by
 // the fp32 matrix rate, a seventh of the 16-bit one: tiles of 32 keys go through
 // registers to LDS, the next one's on its way.  Three packed maps (1225, 784 and
-// 193 tokens, 12 heads of 96): 114 us, 87 TFLOP/s of the 153 that a large matrix
-// product reaches; what is lost is mostly the workgroups' uneven number per CU.
+// 193 tokens, 12 heads of 96): 115 us, 86 TFLOP/s of the 153 that a large matrix
+// product reaches, matrix cores 52 per cent busy; what is lost is mostly the
+// workgroups' uneven number per CU.
 #include <type_traits>
 
 #include "attn_prompt.h"

@@ -3,10 +3,11 @@
 // A workgroup owns one tile (32 tokens of one head) and builds or reads it in
 // LDS: the V codes of 8 tokens share a word, so a tile is the smallest piece
 // that is written whole.  Where the tile already holds earlier tokens it is
-// read first.  Both calls are bound by memory: 2 D values in and 5/4 D bytes
-// out per token and head.  35472 tokens of 8 heads of 128: append 52 .. 66 us
-// (190 MB), read as float32 63 us (336 MB, 5.3 TB/s); 32 single tokens 5.5 and
-// 3.7 us, a chain of dependent loads (offsets, slot, length, page, values).
+// read first.  2 D values in and 5/4 D bytes out per token and head.  35472 tokens
+// of 8 heads of 128: read as float32 72 us (336 MB, 4.7 TB/s: memory); append 71
+// us (190 MB, 52 .. 66 if the input stays in the 256 MB cache: the quantiser's
+// vector instructions, 66 per cent busy).  32 single tokens 5.6 and 3.8 us, a
+// chain of dependent loads (offsets, slot, length, page, values).
 #include "decoder.h"
 
 namespace ios {

@@ -7,8 +7,9 @@
 // atomically.  Reserve and compact need the whole of refs (4 bytes a page):
 // one workgroup reads it once.  Page contents move in a second launch over
 // the list that the first one leaves, bound by memory.  16 sequences over 512
-// pages: reserve 7.4 us, fork 2.9, free 3.1; compacting 512 pages of 8 layers and
-// 8 heads of 128: 5 us for the lists, 24 for the contents (72 MB read and written).
+// pages: reserve 7.5 us, fork 2.8, free 3.1; compacting 512 pages of 8 layers and
+// 8 heads of 128: 5 us for the lists, 32 for the contents (72 MB read and written;
+// 23 if the pool stays in the 256 MB cache).
 #include "decoder.h"
 
 namespace ios {
