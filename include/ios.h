@@ -372,7 +372,10 @@ int ios_device_status(ios_graph *g, void *hip_stream, int32_t *flags);
 /* ------------------------------------- attention and its key-value cache */
 /* Operators of a token decoder that reads what a CNN trunk saw: attention over
  * whole prompts, a paged cache that holds keys and values in 4 bits, single
- * token attention over that cache, and the bookkeeping of its pages.  They
+ * token attention over that cache, and the bookkeeping of its pages; rotation
+ * by positions; and for several tokens a step, attention of a tree of drafted
+ * tokens over the cache, the check of the drafts, and the accepted ones'
+ * place in the cache.  They
  * take no graph: every buffer is the caller's, on the current HIP device, and
  * what changes from call to call (lengths, page tables) stays in device
  * memory, so that a recorded call can be replayed on other lengths.  Every
@@ -438,6 +441,45 @@ int ios_attn_prompt(const ios_attn_desc *d, const ios_tokens *q, const ios_token
                     const ios_tokens *out, float *lse, const int32_t *cu_q, const int32_t *cu_k, void *work,
                     int64_t work_bytes, void *hip_stream);
 
+/* A rotation by positions: pair i of a head's first `dim` values a, b, values
+ * (i, i + dim / 2) or (2 i, 2 i + 1), turns by the angle t freq[i] at position
+ * t.  In 64 bits rounded once (the angle too is one rounded product),
+ *     c = f32(amplitude cos(t freq[i])),  s = f32(amplitude sin(t freq[i]))
+ * (of 10^6 of them a few may be the neighbouring float32 number), then in
+ * float32, each step rounded to nearest even, and to the tensor's type:
+ *     a' = f32(a c) - f32(b s),  b' = f32(a s) + f32(b c).
+ * The other values of a head stay as they are.  freq negated turns back, which
+ * is also the gradient (where the amplitude is 1; times its square if not). */
+typedef struct {
+  int32_t dim;               /* even, from 2 to the head's size                        */
+  int32_t interleaved;       /* 1 = pairs of neighbours, 0 = of halves                 */
+  float amplitude;           /* 1 unless long contexts ask for another; finite         */
+  int32_t reserved;          /* 0                                                      */
+  double freq[64];           /* dim / 2 angles a position, each at most 1024 either way */
+} ios_rotary;
+
+/* Fill r->freq (from r->dim): f_i = base^(-2 i / dim), for contexts `factor`
+ * times as long as those that the model knows divided by `factor`; all of them
+ * where original == 0, and otherwise by how often a pair turns in `original`
+ * positions, n_i = original f_i / (2 pi): those that turn `high` times or more
+ * keep f_i, those that turn `low` times or less are divided, and between them
+ *     freq[i] = f_i (g + (1 - g) / factor),  g = (n_i - low) / (high - low).
+ * A host call; the device is not touched.
+ * Errors: IOS_E_ARG (dim, base <= 1, factor <= 0, original < 0, low >= high
+ * where original > 0). */
+int ios_rotary_freqs(ios_rotary *r, double base, double factor, double original, double low, double high);
+
+/* Turn the rows of q into q_out and those of k into k_out: head_dim values a
+ * head (a multiple of 8 up to 128), `heads` and `kv_heads` of them, row i at
+ * position pos[i] (device array; negative positions turn the other way).  An
+ * output may be its input itself (the same address and strides) or lie apart
+ * from every input.  k and k_out may both be NULL.
+ * Errors: IOS_E_ARG, IOS_E_SHAPE (other lengths), IOS_E_UNSUPPORTED
+ * (head_dim), IOS_E_HIP. */
+int ios_rotate(const ios_rotary *r, int32_t dtype, int32_t head_dim, const ios_tokens *q, const ios_tokens *q_out,
+               int32_t heads, const ios_tokens *k, const ios_tokens *k_out, int32_t kv_heads, const int32_t *pos,
+               void *hip_stream);
+
 /* A paged key-value cache.  A page holds page_tokens consecutive tokens of a
  * sequence, of every layer and head; a sequence is a slot of the table, which
  * lists its pages in order; pages can be shared (refs counts the rows that
@@ -489,6 +531,27 @@ int ios_cache_reserve(const ios_cache *c, int32_t n, const int32_t *seqs, const 
 int ios_cache_append(const ios_cache *c, int32_t layer, int32_t dtype, const ios_tokens *k, const ios_tokens *v,
                      int32_t n, const int32_t *seqs, const int32_t *cu, void *hip_stream);
 
+/* The same with positions: every key is turned by its token's place in the
+ * sequence (0 for its first) on the way in, and the rows of q (`heads` heads)
+ * by the same into q_out; both may be NULL.  Leaves in q_out and the cache,
+ * to the bit, what ios_rotate and ios_cache_append leave.  Rows of q that
+ * belong to no token of the cache are not written; q_out may be q itself or
+ * lie apart from every input.
+ * Errors: as ios_cache_append and ios_rotate. */
+int ios_cache_append_rotary(const ios_cache *c, int32_t layer, int32_t dtype, const ios_rotary *r, const ios_tokens *q,
+                            const ios_tokens *q_out, int32_t heads, const ios_tokens *k, const ios_tokens *v, int32_t n,
+                            const int32_t *seqs, const int32_t *cu, void *hip_stream);
+
+/* Write accepted drafts to one layer: rows path[i * max_path + j] of k and v,
+ * j = 0 .. count[i]-1, become the last tokens of sequence seqs[i] (device
+ * arrays, as ios_verify leaves them; after ios_cache_reserve of count[i]; keys
+ * are written as they are).  1 <= max_path <= 64, and a count is clipped to 0 ..
+ * max_path.  Where there are more rows than the sequence has tokens, the first
+ * are dropped; a row outside k and v makes its token 0.
+ * Errors: as ios_cache_append. */
+int ios_cache_keep(const ios_cache *c, int32_t layer, int32_t dtype, const ios_tokens *k, const ios_tokens *v, int32_t n,
+                   const int32_t *seqs, const int32_t *path, int32_t max_path, const int32_t *count, void *hip_stream);
+
 /* Read the same tokens back, as the values they are held as (cu[i+1] - cu[i]
  * = the sequence's length reads all of it; rows for which there is no token
  * are 0).  Errors: as ios_cache_append. */
@@ -503,6 +566,23 @@ int ios_cache_read(const ios_cache *c, int32_t layer, int32_t dtype, const ios_t
 int ios_attn_cache(const ios_cache *c, int32_t layer, const ios_attn_desc *d, const ios_tokens *q,
                    const ios_tokens *out, float *lse, const int32_t *seqs, void *work, int64_t work_bytes,
                    void *hip_stream);
+
+/* Attention of drafted tokens: rows cu[i] .. cu[i+1]-1 of q, k, v and out are
+ * drafts behind sequence seqs[i] (< 0: of none), at most max_drafts <= 64 of
+ * them (rows past that are not written).  parent[row] is the place of the
+ * row's parent among its sequence's drafts; one that is not an earlier draft's
+ * (-1, say) is none.  A row sees every token that the layer holds of the
+ * sequence, its ancestors and itself; a draft that it does not see never
+ * changes it, not even by a NaN.  Nothing is written to the cache.  lse as
+ * ios_attn_prompt, [heads][q->tokens]; causal is not read.  Drafts' keys and
+ * values are read as they are, cached ones as they are held.  `work` (of
+ * work_bytes) may be NULL; it needs no initial values, and
+ * ios_attn_tree_work_bytes says how much spreads long caches over workgroups.
+ * Errors: as ios_attn_cache. */
+int ios_attn_tree_work_bytes(const ios_attn_desc *d, int64_t q_tokens, int32_t max_drafts, int64_t *bytes);
+int ios_attn_tree(const ios_cache *c, int32_t layer, const ios_attn_desc *d, const ios_tokens *q, const ios_tokens *k,
+                  const ios_tokens *v, const ios_tokens *out, float *lse, const int32_t *seqs, const int32_t *cu,
+                  const int32_t *parent, int32_t max_drafts, void *work, int64_t work_bytes, void *hip_stream);
 
 /* children[i] becomes a second sequence with the tokens of parents[i], sharing
  * its pages (device arrays; children are distinct empty slots, no parent is
@@ -530,6 +610,54 @@ int ios_cache_copy(const ios_cache *c, int32_t n, const int32_t *src, const int3
  * table entries, bit 2 = ios_cache_fork met a child in use.
  * Errors: IOS_E_ARG, IOS_E_HIP. */
 int ios_cache_status(const ios_cache *c, void *hip_stream, int32_t *flags);
+
+/* A [rows][vocab] matrix of probabilities on the device, row_stride elements
+ * from row to row, aligned as its elements are. */
+typedef struct {
+  void *data;
+  int64_t rows;
+  int64_t row_stride;
+} ios_rows;
+
+/* A check of drafts. */
+typedef struct {
+  int32_t dtype;             /* IOS_F32 / F16 / BF16, of p and q                       */
+  int32_t seqs;              /* sequences of the call                                  */
+  int32_t vocab;
+  int32_t max_drafts;        /* rows of a sequence that are looked at, 1 to 64         */
+} ios_verify_desc;
+
+/* Bytes of the workspace; it needs no initial values, and nothing in it has to
+ * be kept between calls.  Errors: IOS_E_ARG. */
+int ios_verify_work_bytes(const ios_verify_desc *d, int64_t *bytes);
+
+/* Which drafted tokens stand, so that accepted tokens are distributed as the
+ * model's own.  Sequence i has rows cu[i] .. cu[i+1]-1: row 0 is the token that
+ * is certain, the others are drafts with tokens[row] and parent[row] (places
+ * among the sequence's rows, as ios_attn_tree; a row whose parent is not an
+ * earlier one, or whose token is not below vocab, is passed over).  p[row] are
+ * the model's probabilities for what follows the row, q[row] the draft's, of
+ * which the row's children were drawn one by one; q NULL: they were certain.
+ *
+ * Row 0 is the first node.  The node's children are tried in their order: with
+ * C = 0 and S = 1, a child of token x stands where
+ *     accept[child] S q(x) < max(p(x) - C q(x), 0),
+ * and is the next node; where it does not, C grows by S, then S becomes the sum
+ * of max(p - C q, 0) over the vocabulary (if S is 0 both stay).  Without q it
+ * stands where accept[child] S < p(x), and where it does not S shrinks by p(x)
+ * and p(x) counts as 0 from there on.  Where no child stands, the next token is
+ * the first whose running sum of what is left (of p, if that is all 0) passes
+ * sample[i] times the whole sum.  accept [rows] and sample [seqs] are uniform
+ * numbers of [0, 1).  All of it is in 64 bits, in an order of sums that does
+ * not change; probabilities that are negative, infinite or NaN count as 0.
+ *
+ * path[i * max_drafts + j] receives the rows that stand, row 0 first and -1
+ * behind them, count[i] their number, next[i] the next token (-1 where no
+ * probability is above 0).  A sequence without rows has 0, and -1 as its next.
+ * Errors: IOS_E_ARG, IOS_E_SHAPE (p and q of other lengths), IOS_E_HIP. */
+int ios_verify(const ios_verify_desc *d, const ios_rows *p, const ios_rows *q, const int32_t *tokens,
+               const int32_t *parent, const int32_t *cu, const float *accept, const float *sample, int32_t *path,
+               int32_t *count, int32_t *next, void *work, int64_t work_bytes, void *hip_stream);
 
 /* Message describing the calling thread's most recent error. */
 const char *ios_last_error(void);

@@ -61,7 +61,8 @@ EXPORTED = ["ios_graph_create", "ios_graph_destroy", "ios_add_input", "ios_add_o
             "ios_attn_work_bytes", "ios_attn_prompt", "ios_attn_cache",
             "ios_cache_page_bytes", "ios_cache_work_bytes", "ios_cache_reserve", "ios_cache_append",
             "ios_cache_read", "ios_cache_fork", "ios_cache_free", "ios_cache_compact", "ios_cache_copy",
-            "ios_cache_status", "ios_last_error"]
+            "ios_cache_status", "ios_rotary_freqs", "ios_rotate", "ios_cache_append_rotary", "ios_cache_keep",
+            "ios_attn_tree_work_bytes", "ios_attn_tree", "ios_verify_work_bytes", "ios_verify", "ios_last_error"]
 
 
 class IosError(RuntimeError):
@@ -100,6 +101,25 @@ class ios_cache(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("pool", "refs", "table", "lens", "work")]
 
 
+class ios_rotary(ctypes.Structure):
+    """A rotation by positions; ios_rotary_freqs fills freq."""
+    _fields_ = [("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("freq", ctypes.c_double * 64)]
+
+    def __init__(self, dim: int = 0, interleaved: int = 0, amplitude: float = 1.0):
+        super().__init__(dim, interleaved, amplitude, 0)
+
+
+class ios_rows(ctypes.Structure):
+    """A [rows][vocab] device matrix: address, rows, and the stride of a row in
+    elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class ios_verify_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "seqs", "vocab", "max_drafts")]
+
+
 COST_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64,
                            ctypes.POINTER(ctypes.c_int32), ctypes.c_int32, ctypes.c_int32,
                            ctypes.POINTER(ctypes.c_int64))
@@ -108,6 +128,7 @@ _P = ctypes.c_void_p
 _i32, _i64 = ctypes.c_int32, ctypes.c_int64
 _pi32, _pi64 = ctypes.POINTER(_i32), ctypes.POINTER(_i64)
 _pf = ctypes.POINTER(ctypes.c_float)
+_pr, _pm, _pv = ctypes.POINTER(ios_rotary), ctypes.POINTER(ios_rows), ctypes.POINTER(ios_verify_desc)
 _pt, _pd, _pc = ctypes.POINTER(ios_tokens), ctypes.POINTER(ios_attn_desc), ctypes.POINTER(ios_cache)
 
 _sig = {
@@ -152,6 +173,14 @@ _sig = {
     "ios_cache_compact": (ctypes.c_int, [_pc, _P, _P]),
     "ios_cache_copy": (ctypes.c_int, [_pc, _i32, _P, _P, _P]),
     "ios_cache_status": (ctypes.c_int, [_pc, _P, _pi32]),
+    "ios_rotary_freqs": (ctypes.c_int, [_pr] + [ctypes.c_double] * 5),
+    "ios_rotate": (ctypes.c_int, [_pr, _i32, _i32, _pt, _pt, _i32, _pt, _pt, _i32, _P, _P]),
+    "ios_cache_append_rotary": (ctypes.c_int, [_pc, _i32, _i32, _pr, _pt, _pt, _i32, _pt, _pt, _i32, _P, _P, _P]),
+    "ios_cache_keep": (ctypes.c_int, [_pc, _i32, _i32, _pt, _pt, _i32, _P, _P, _i32, _P, _P]),
+    "ios_attn_tree_work_bytes": (ctypes.c_int, [_pd, _i64, _i32, _pi64]),
+    "ios_attn_tree": (ctypes.c_int, [_pc, _i32, _pd, _pt, _pt, _pt, _pt, _P, _P, _P, _P, _i32, _P, _i64, _P]),
+    "ios_verify_work_bytes": (ctypes.c_int, [_pv, _pi64]),
+    "ios_verify": (ctypes.c_int, [_pv, _pm, _pm, _P, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
     "ios_last_error": (ctypes.c_char_p, []),
 }
 for _name, (_res, _args) in _sig.items():
@@ -433,6 +462,53 @@ def ios_cache_status(c: ios_cache, stream: int = 0) -> int:
     f = _i32()
     _check(_lib.ios_cache_status(c, stream or None, ctypes.byref(f)))
     return f.value
+
+
+def ios_rotary_freqs(r: ios_rotary, base: float, factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                     high: float = 4.0) -> None:
+    _check(_lib.ios_rotary_freqs(r, base, factor, original, low, high))
+
+
+def ios_rotate(r: ios_rotary, dtype: int, head_dim: int, q: ios_tokens, q_out: ios_tokens, heads: int,
+               k: Optional[ios_tokens], k_out: Optional[ios_tokens], kv_heads: int, pos: int, stream: int = 0) -> None:
+    _check(_lib.ios_rotate(r, dtype, head_dim, q, q_out, heads, k, k_out, kv_heads, pos, stream or None))
+
+
+def ios_cache_append_rotary(c: ios_cache, layer: int, dtype: int, r: ios_rotary, q: Optional[ios_tokens],
+                            q_out: Optional[ios_tokens], heads: int, k: ios_tokens, v: ios_tokens, n: int, seqs: int,
+                            cu: int, stream: int = 0) -> None:
+    _check(_lib.ios_cache_append_rotary(c, layer, dtype, r, q, q_out, heads, k, v, n, seqs, cu, stream or None))
+
+
+def ios_cache_keep(c: ios_cache, layer: int, dtype: int, k: ios_tokens, v: ios_tokens, n: int, seqs: int, path: int,
+                   max_path: int, count: int, stream: int = 0) -> None:
+    _check(_lib.ios_cache_keep(c, layer, dtype, k, v, n, seqs, path, max_path, count, stream or None))
+
+
+def ios_attn_tree_work_bytes(d: ios_attn_desc, q_tokens: int, max_drafts: int) -> int:
+    n = _i64()
+    _check(_lib.ios_attn_tree_work_bytes(ctypes.byref(d), q_tokens, max_drafts, ctypes.byref(n)))
+    return n.value
+
+
+def ios_attn_tree(c: ios_cache, layer: int, d: ios_attn_desc, q: ios_tokens, k: ios_tokens, v: ios_tokens,
+                  out: ios_tokens, lse: int, seqs: int, cu: int, parent: int, max_drafts: int, work: int = 0,
+                  work_bytes: int = 0, stream: int = 0) -> None:
+    _check(_lib.ios_attn_tree(c, layer, d, q, k, v, out, lse or None, seqs, cu, parent, max_drafts, work or None,
+                              work_bytes, stream or None))
+
+
+def ios_verify_work_bytes(d: ios_verify_desc) -> int:
+    n = _i64()
+    _check(_lib.ios_verify_work_bytes(ctypes.byref(d), ctypes.byref(n)))
+    return n.value
+
+
+def ios_verify(d: ios_verify_desc, p: ios_rows, q: Optional[ios_rows], tokens: int, parent: int, cu: int, accept: int,
+               sample: int, path: int, count: int, next: int, work: int = 0, work_bytes: int = 0,
+               stream: int = 0) -> None:
+    _check(_lib.ios_verify(d, p, q, tokens, parent, cu, accept, sample, path, count, next, work or None, work_bytes,
+                           stream or None))
 
 
 def ios_last_error() -> str:

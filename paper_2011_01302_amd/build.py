@@ -32,7 +32,8 @@ SOURCES = ["stage_kernel_full.hip", "stage_kernel_full_persist.hip", "stage_kern
            "stage_kernel_sepsplit_persist.hip",
            "stage_kernel_pipe.hip", "stage_kernel_pipe_persist.hip", "stage_kernel_light.hip",
            "stage_kernel_light_persist.hip",
-           "attn_prompt.hip", "attn_prompt_float.hip", "attn_cache.hip", "cache.hip", "pages.hip",
+           "attn_prompt.hip", "attn_prompt_float.hip", "attn_cache.hip", "attn_tree.hip", "cache.hip", "pages.hip",
+           "rotate.hip", "verify.hip",
            "noalloc.hip", "pack.hip", "graph.cpp", "sched.cpp", "exec.cpp", "api.cpp", "decoder.cpp",
            "stage_launch.cpp"]
 

@@ -1,4 +1,4 @@
-// Keys and values to and from the 4-bit cache (ios_cache_append, ios_cache_read).
+// Keys and values to and from the 4-bit cache (ios_cache_append, ios_cache_append_rotary, ios_cache_keep, ios_cache_read).
 //
 // A workgroup owns one tile (32 tokens of one head) and builds or reads it in
 // LDS: the V codes of 8 tokens share a word, so a tile is the smallest piece
@@ -8,7 +8,7 @@
 // us (190 MB, 52 .. 66 if the input stays in the 256 MB cache: the quantiser's
 // vector instructions, 66 per cent busy).  32 single tokens 5.6 and 3.8 us, a
 // chain of dependent loads (offsets, slot, length, page, values).
-#include "decoder.h"
+#include "rotary.h"
 
 namespace ios {
 
@@ -18,22 +18,21 @@ constexpr float kLimit = 61440.f;       // so that z + s c never leaves f16
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 
 template <class T>
-struct alignas(16) Row8 {
-  T v[8];
-};
+using Row8 = Octet8<T>;
 
 // What both kernels need to know of the tile of this workgroup.
 struct TileJob {
   unsigned char *tile;        // null: nothing to do
   int lo, hi;                 // tokens of the tile in the call, [lo, hi)
   int64_t row;                // row of the call that is the tile's token 0 (may be negative)
+  int pos;                    // place of the tile's token 0 in the sequence
 };
 
 // Sequence i has tiles from unit cu[i] / 32 + 2 i on: L tokens touch at most
 // L / 32 + 2 tiles.
 __device__ __forceinline__ TileJob find_tile(const CacheView &c, int tile_b, int n, const int32_t *seqs,
                                              const int32_t *cu, int64_t tokens, int head, int *seq) {
-  TileJob j{nullptr, 0, 0, 0};
+  TileJob j{nullptr, 0, 0, 0, 0};
   auto start = [&](int i) { return clip(cu[i], tokens) / kTileKeys + 2 * (int64_t)i; };
   const int i = find_owner(n, blockIdx.x, start);
   *seq = i;
@@ -47,6 +46,24 @@ __device__ __forceinline__ TileJob find_tile(const CacheView &c, int tile_b, int
   j.lo = p0 > t0 ? (int)(p0 - t0) : 0;
   j.hi = len - t0 < kTileKeys ? (int)(len - t0) : kTileKeys;
   j.row = a + t0 - first;
+  j.pos = (int)t0;
+  return j;
+}
+
+// The same for the accepted drafts of sequence i, rows path[i * most ..] of the call: `per` tiles for every sequence.
+// j.row is then the place in the list that is the tile's token 0.
+__device__ __forceinline__ TileJob find_kept(const CacheView &c, int tile_b, int n, const int32_t *seqs,
+                                             const int32_t *count, int most, int head, int *seq) {
+  TileJob j{nullptr, 0, 0, 0, 0};
+  const int per = most / kTileKeys + 2, i = blockIdx.x / per;
+  *seq = i;
+  const int slot = seqs[i], len = cache_len(c, slot), kept = (int)clip(count[i], most), first = len - kept;
+  const int p0 = max(first, 0), t0 = (p0 / kTileKeys + (int)blockIdx.x % per) * kTileKeys;
+  if (kept == 0 || t0 >= len) return j;
+  j.tile = cache_tile(c, slot, t0, head, tile_b);
+  j.lo = max(p0 - t0, 0);
+  j.hi = min(len - t0, kTileKeys);
+  j.row = t0 - first;
   return j;
 }
 
@@ -99,25 +116,101 @@ __device__ __forceinline__ Quant quantise(const Row8<T> &r) {
   return q;
 }
 
-template <class T, int G>
+// Where a call's tokens come from: rows behind each other, the same with keys to be turned and queries beside them, or
+// rows by a list.
+enum { ROWS = 0, TURNED = 1, KEPT = 2 };
+template <int M> struct Source {};
+template <> struct Source<TURNED> {
+  ios_rotary r;
+  ios_tokens q, qo;
+  int heads;
+};
+template <> struct Source<KEPT> {
+  const int32_t *count;
+  int most;
+};
+constexpr int kQueryHeads = 4;          // heads of queries that a workgroup turns
+
+// The queries of a tile's tokens, up to kQueryHeads heads from head0 on.
+template <class T>
+__device__ __forceinline__ void turn_queries(const Source<TURNED> &x, const TileJob &j, int dim, int head0) {
+  __shared__ float2 cs[kTileKeys * kMaxPairs];
+  const RotaryUnits u(x.r, dim);
+  const int heads = min(x.heads - head0, kQueryHeads), keys = j.hi - j.lo;
+  for (int y = threadIdx.x; y < keys * u.half; y += 256)
+    cs[y] = turn_of(j.pos + j.lo + y / u.half, x.r.freq[y % u.half], x.r.amplitude);
+  __syncthreads();
+  for (int y = threadIdx.x; y < keys * heads * u.all; y += 256) {
+    const int row = y / u.all, at = y - row * u.all, key = row / heads, h = head0 + row - key * heads;
+    const int64_t t = j.row + j.lo + key;
+    RotaryUnit<T> unit;
+    unit.load(u, (const T *)x.q.data + t * x.q.token_stride + h * x.q.head_stride, at);
+    unit.turn_by(u, cs + key * u.half, at);
+    unit.store(u, (T *)x.qo.data + t * x.qo.token_stride + h * x.qo.head_stride, at);
+  }
+}
+
+// The tile's keys, octet tid + 256 u of them in kr[u].
+template <class T, int G, int N>
+__device__ __forceinline__ void turn_keys(const ios_rotary &r, const TileJob &j, Row8<T> (&kr)[N]) {
+  __shared__ __align__(16) T rows[kTileKeys * 32 * G];
+  __shared__ float2 cs[kTileKeys * kMaxPairs];
+  const RotaryUnits u(r, 32 * G);
+  const int tid = threadIdx.x, keys = j.hi - j.lo;
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (tid + 256 * e < kTileKeys * 4 * G) *(Row8<T> *)(rows + (tid + 256 * e) * 8) = kr[e];
+  for (int y = tid; y < keys * u.half; y += 256)
+    cs[y] = turn_of(j.pos + j.lo + y / u.half, r.freq[y % u.half], r.amplitude);
+  __syncthreads();
+  for (int y = tid; y < keys * u.turned; y += 256) {
+    const int key = y / u.turned, at = y - key * u.turned;
+    T *row = rows + (j.lo + key) * 32 * G;
+    RotaryUnit<T> unit;
+    unit.load(u, row, at);
+    unit.turn_by(u, cs + key * u.half, at);
+    unit.store(u, row, at);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (tid + 256 * e < kTileKeys * 4 * G) kr[e] = *(const Row8<T> *)(rows + (tid + 256 * e) * 8);
+}
+
+// For M == KEPT `cu` is the list of rows.
+template <class T, int G, int M>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, ios_tokens k, ios_tokens v, int n,
-                                                           const int32_t *seqs, const int32_t *cu) {
+                                                           const int32_t *seqs, const int32_t *cu, Source<M> from) {
   __shared__ uint32_t img[tile_bytes(G) / 4];
   __shared__ uint32_t vc[kTileKeys * 4 * G];                 // codes of V by key and octet of values
   const int tid = threadIdx.x, head = blockIdx.y;
   int seq;
-  const TileJob j = find_tile(c, tile_bytes(G), n, seqs, cu, k.tokens, head, &seq);
-  if (!j.tile || j.lo >= j.hi) return;
+  TileJob j;
+  if constexpr (M == KEPT) j = find_kept(c, tile_bytes(G), n, seqs, from.count, from.most, head, &seq);
+  else j = find_tile(c, tile_bytes(G), n, seqs, cu, k.tokens, M == TURNED ? min(head, c.heads - 1) : head, &seq);
+  if ((!j.tile && !(M == TURNED && head >= c.heads)) || j.lo >= j.hi) return;
+  if constexpr (M == TURNED) {
+    if (head >= c.heads) {
+      turn_queries<T>(from, j, 32 * G, (head - c.heads) * kQueryHeads);
+      return;
+    }
+  }
   // every load first: the tokens' values (a thread has up to N octets of K and of V) and the tile, if it holds some
   constexpr int N = (kTileKeys * 4 * G + 255) / 256;
   Row8<T> kr[N], vr[N];
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int o = tid + 256 * u, key = min(max(o / (4 * G), j.lo), j.hi - 1), oct = o % (4 * G);
-    const int64_t row = j.row + key;
+    int64_t row = j.row + key;
+    if constexpr (M == KEPT) row = cu[(int64_t)seq * from.most + row];
+    if (M == KEPT && (row < 0 || row >= k.tokens)) {         // no such row: the token is 0
+      kr[u] = vr[u] = Row8<T>{};
+      continue;
+    }
     kr[u] = *(const Row8<T> *)((const T *)k.data + row * k.token_stride + head * k.head_stride + oct * 8);
     vr[u] = *(const Row8<T> *)((const T *)v.data + row * v.token_stride + head * v.head_stride + oct * 8);
   }
+  if constexpr (M == TURNED) turn_keys<T, G, N>(from.r, j, kr);
   uintx4 *gt = (uintx4 *)j.tile, *li = (uintx4 *)img;
   for (int i = tid; i < tile_bytes(G) / 16; i += 256) li[i] = j.lo > 0 ? gt[i] : uintx4{0, 0, 0, 0};
   __syncthreads();
@@ -213,27 +306,55 @@ hipError_t for_type(int dtype, F f) {
   return f(__bf16{});
 }
 
-}  // namespace
+// The tiles that the tokens of n sequences can touch.
+unsigned tiles_of(int64_t tokens, int n) { return (unsigned)(tokens / kTileKeys + 2 * (int64_t)n); }
 
-#define IOS_FOR_GROUPS(kernel)                                                                          \
-  for_type(dtype, [&](auto t) {                                                                         \
-    using T = decltype(t);                                                                              \
-    const dim3 grid((unsigned)(k.tokens / kTileKeys + 2 * (int64_t)n), c.heads);                        \
-    if (groups == 1) hipLaunchKernelGGL((kernel<T, 1>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu);   \
-    else if (groups == 2) hipLaunchKernelGGL((kernel<T, 2>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu); \
-    else if (groups == 3) hipLaunchKernelGGL((kernel<T, 3>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu); \
-    else hipLaunchKernelGGL((kernel<T, 4>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu);               \
-    return hipGetLastError();                                                                           \
-  })
+template <int M>
+hipError_t append(const CacheView &c, int groups, int dtype, dim3 grid, const ios_tokens &k, const ios_tokens &v, int n,
+                  const int32_t *seqs, const int32_t *cu, const Source<M> &from, hipStream_t s) {
+  return for_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (groups == 1) hipLaunchKernelGGL((cache_append_kernel<T, 1, M>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu, from);
+    else if (groups == 2) hipLaunchKernelGGL((cache_append_kernel<T, 2, M>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu, from);
+    else if (groups == 3) hipLaunchKernelGGL((cache_append_kernel<T, 3, M>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu, from);
+    else hipLaunchKernelGGL((cache_append_kernel<T, 4, M>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu, from);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace
 
 hipError_t launch_append(const CacheView &c, int groups, int dtype, const ios_tokens &k, const ios_tokens &v, int n,
                          const int32_t *seqs, const int32_t *cu, hipStream_t s) {
-  return IOS_FOR_GROUPS(cache_append_kernel);
+  return append<ROWS>(c, groups, dtype, dim3(tiles_of(k.tokens, n), c.heads), k, v, n, seqs, cu, {}, s);
+}
+
+hipError_t launch_append_rotary(const CacheView &c, int groups, int dtype, const ios_rotary &r, const ios_tokens *q,
+                                const ios_tokens *qo, int heads, const ios_tokens &k, const ios_tokens &v, int n,
+                                const int32_t *seqs, const int32_t *cu, hipStream_t s) {
+  Source<TURNED> from{r, {}, {}, 0};
+  if (q) from.q = *q, from.qo = *qo, from.heads = heads;
+  const dim3 grid(tiles_of(k.tokens, n), c.heads + (from.heads + kQueryHeads - 1) / kQueryHeads);
+  return append<TURNED>(c, groups, dtype, grid, k, v, n, seqs, cu, from, s);
+}
+
+hipError_t launch_keep(const CacheView &c, int groups, int dtype, const ios_tokens &k, const ios_tokens &v, int n,
+                       const int32_t *seqs, const int32_t *path, int most, const int32_t *count, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)n * (most / kTileKeys + 2)), c.heads);
+  return append<KEPT>(c, groups, dtype, grid, k, v, n, seqs, path, {count, most}, s);
 }
 
 hipError_t launch_read(const CacheView &c, int groups, int dtype, const ios_tokens &k, const ios_tokens &v, int n,
                        const int32_t *seqs, const int32_t *cu, hipStream_t s) {
-  return IOS_FOR_GROUPS(cache_read_kernel);
+  return for_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    const dim3 grid(tiles_of(k.tokens, n), c.heads);
+    if (groups == 1) hipLaunchKernelGGL((cache_read_kernel<T, 1>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu);
+    else if (groups == 2) hipLaunchKernelGGL((cache_read_kernel<T, 2>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu);
+    else if (groups == 3) hipLaunchKernelGGL((cache_read_kernel<T, 3>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu);
+    else hipLaunchKernelGGL((cache_read_kernel<T, 4>), grid, dim3(256), 0, s, c, k, v, n, seqs, cu);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace ios

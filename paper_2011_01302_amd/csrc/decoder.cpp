@@ -1,6 +1,7 @@
 // Entry points of the decoder operators (declared and documented in ios.h):
 // every size, pointer and alignment that the host can see is checked here,
 // before anything is launched.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -135,6 +136,57 @@ int usable(int splits, int64_t rows, const ios_attn_desc &d, const void *work, i
   return splits;
 }
 
+// A rotation of heads of this size.
+void check_rotary(const ios_rotary *r, int head_dim) {
+  need(r != nullptr, IOS_E_ARG, "null rotation");
+  need(r->dim >= 2 && r->dim % 2 == 0 && r->dim <= head_dim, IOS_E_ARG, "a rotation's dim must be even, from 2 to head_dim");
+  need(r->interleaved == 0 || r->interleaved == 1, IOS_E_ARG, "interleaved must be 0 or 1");
+  need(r->reserved == 0, IOS_E_ARG, "reserved must be 0");
+  need(std::isfinite(r->amplitude), IOS_E_ARG, "amplitude must be finite");
+  for (int i = 0; i < r->dim / 2; ++i)
+    need(std::fabs(r->freq[i]) <= 1024.0, IOS_E_ARG, "a frequency must be within 1024");   // not a NaN's either
+}
+
+// An output that is its input or lies apart.
+void check_turned(const ios_tokens *in, const ios_tokens *out, int dtype, int heads, const char *what) {
+  check_tokens(in, dtype, what);
+  check_out(out, dtype, heads, what);
+  const std::string w(what);
+  if (heads < 1 || heads > kMaxHeads) fail(IOS_E_ARG, w + ": head count out of range");
+  if (in->tokens != out->tokens) fail(IOS_E_SHAPE, w + ": input and output have different lengths");
+  if (in->data == out->data && in->data && (in->token_stride != out->token_stride || in->head_stride != out->head_stride))
+    fail(IOS_E_ARG, w + ": in place, the strides must be the same");
+}
+
+// A cache, a type and the tensors that go into one of its layers.
+void check_append(const ios_cache *c, int32_t dtype, const ios_tokens *k, const ios_tokens *v) {
+  check_type(dtype);
+  check_tokens(k, dtype, "k");
+  check_tokens(v, dtype, "v");
+  need(k->tokens == v->tokens, IOS_E_SHAPE, "k and v have different lengths");
+}
+
+void check_drafts(int32_t most) {
+  need(most >= 1 && most <= kMaxDrafts, IOS_E_ARG, "drafts of a sequence must be 1 to 64");
+}
+
+void check_rows(const ios_rows *t, const ios_verify_desc *d, const char *what) {
+  const std::string w(what);
+  if (!t) fail(IOS_E_ARG, w + ": null matrix");
+  if (t->rows < 0 || t->rows > kMaxTokens) fail(IOS_E_ARG, w + ": rows out of range");
+  if (t->rows > 0 && !t->data) fail(IOS_E_ARG, w + ": null data");
+  if (reinterpret_cast<uintptr_t>(t->data) % type_size(d->dtype)) fail(IOS_E_ARG, w + ": misaligned data");
+  if (t->row_stride < 0 || t->row_stride > ((int64_t)1 << 32)) fail(IOS_E_ARG, w + ": stride out of range");
+}
+
+void check_verify(const ios_verify_desc *d) {
+  need(d != nullptr, IOS_E_ARG, "null descriptor");
+  check_type(d->dtype);
+  need(d->seqs >= 1 && d->seqs <= kMaxAttnSeqs, IOS_E_ARG, "seqs out of range");
+  need(d->vocab >= 1, IOS_E_ARG, "vocab out of range");
+  check_drafts(d->max_drafts);
+}
+
 int move_tokens(bool read, const ios_cache *c, int32_t layer, int32_t dtype, const ios_tokens *k, const ios_tokens *v,
                 int32_t n, const int32_t *seqs, const int32_t *cu, void *hip_stream) {
   return guarded([&] {
@@ -240,6 +292,151 @@ extern "C" int ios_cache_read(const ios_cache *c, int32_t layer, int32_t dtype, 
                               const ios_tokens *v, int32_t n, const int32_t *seqs, const int32_t *cu,
                               void *hip_stream) {
   return move_tokens(true, c, layer, dtype, k, v, n, seqs, cu, hip_stream);
+}
+
+extern "C" int ios_rotary_freqs(ios_rotary *r, double base, double factor, double original, double low, double high) {
+  return guarded([&] {
+    need(r != nullptr, IOS_E_ARG, "null rotation");
+    need(r->dim >= 2 && r->dim % 2 == 0 && r->dim <= 128, IOS_E_ARG, "a rotation's dim must be even, from 2 to 128");
+    need(base > 1.0 && std::isfinite(base), IOS_E_ARG, "base must be above 1");
+    need(factor > 0.0 && std::isfinite(factor), IOS_E_ARG, "factor must be above 0");
+    need(original >= 0.0 && std::isfinite(original), IOS_E_ARG, "original must not be negative");
+    need(original == 0.0 || (low < high && std::isfinite(low) && std::isfinite(high)), IOS_E_ARG, "low must be below high");
+    double f[64];
+    for (int i = 0; i < r->dim / 2; ++i) {
+      f[i] = std::pow(base, -2.0 * i / r->dim);
+      double keep = 0.0;
+      if (original > 0.0) keep = std::min(std::max((original * f[i] / (2 * M_PI) - low) / (high - low), 0.0), 1.0);
+      f[i] = original > 0.0 ? f[i] * (keep + (1.0 - keep) / factor) : f[i] / factor;
+      need(f[i] <= 1024.0, IOS_E_ARG, "factor makes a frequency above 1024");
+    }
+    std::copy(f, f + r->dim / 2, r->freq);
+  });
+}
+
+extern "C" int ios_rotate(const ios_rotary *r, int32_t dtype, int32_t head_dim, const ios_tokens *q,
+                          const ios_tokens *q_out, int32_t heads, const ios_tokens *k, const ios_tokens *k_out,
+                          int32_t kv_heads, const int32_t *pos, void *hip_stream) {
+  return guarded([&] {
+    check_type(dtype);
+    need(head_dim >= 1, IOS_E_ARG, "head_dim out of range");
+    need(head_dim % 8 == 0 && head_dim <= 128, IOS_E_UNSUPPORTED, "head_dim must be a multiple of 8 up to 128");
+    check_rotary(r, head_dim);
+    check_turned(q, q_out, dtype, heads, "q");
+    const ios_tokens none{};
+    need(!k == !k_out, IOS_E_ARG, "k and k_out must be given together");
+    if (k) {
+      check_turned(k, k_out, dtype, kv_heads, "k");
+      need(k->tokens == q->tokens, IOS_E_SHAPE, "q and k have different lengths");
+    }
+    if (q->tokens == 0) return;
+    need(pos != nullptr, IOS_E_ARG, "null positions");
+    launched(launch_rotate(*r, dtype, head_dim, *q, *q_out, heads, k ? *k : none, k ? *k_out : none, k ? kv_heads : 0, pos,
+                           (hipStream_t)hip_stream),
+             "ios_rotate");
+  });
+}
+
+extern "C" int ios_cache_append_rotary(const ios_cache *c, int32_t layer, int32_t dtype, const ios_rotary *r,
+                                       const ios_tokens *q, const ios_tokens *q_out, int32_t heads, const ios_tokens *k,
+                                       const ios_tokens *v, int32_t n, const int32_t *seqs, const int32_t *cu,
+                                       void *hip_stream) {
+  return guarded([&] {
+    check_list(c, n, seqs, cu);
+    check_append(c, dtype, k, v);
+    check_rotary(r, c->head_dim);
+    need(!q == !q_out, IOS_E_ARG, "q and q_out must be given together");
+    if (q) {
+      check_turned(q, q_out, dtype, heads, "q");
+      need(q->tokens == k->tokens, IOS_E_SHAPE, "q and k have different lengths");
+    }
+    const CacheView cv = view(*c, layer);
+    if (n == 0 || k->tokens == 0) return;
+    launched(launch_append_rotary(cv, c->head_dim / kGroup, dtype, *r, q, q_out, heads, *k, *v, n, seqs, cu,
+                                  (hipStream_t)hip_stream),
+             "ios_cache_append_rotary");
+  });
+}
+
+extern "C" int ios_cache_keep(const ios_cache *c, int32_t layer, int32_t dtype, const ios_tokens *k, const ios_tokens *v,
+                              int32_t n, const int32_t *seqs, const int32_t *path, int32_t max_path,
+                              const int32_t *count, void *hip_stream) {
+  return guarded([&] {
+    check_list(c, n, seqs, path);
+    check_append(c, dtype, k, v);
+    check_drafts(max_path);
+    need(n == 0 || count != nullptr, IOS_E_ARG, "null list");
+    const CacheView cv = view(*c, layer);
+    if (n == 0) return;
+    launched(launch_keep(cv, c->head_dim / kGroup, dtype, *k, *v, n, seqs, path, max_path, count, (hipStream_t)hip_stream),
+             "ios_cache_keep");
+  });
+}
+
+extern "C" int ios_attn_tree_work_bytes(const ios_attn_desc *d, int64_t q_tokens, int32_t max_drafts, int64_t *bytes) {
+  return guarded([&] {
+    check_desc(d);
+    check_drafts(max_drafts);
+    need(bytes != nullptr, IOS_E_ARG, "null bytes");
+    need(q_tokens >= 0 && q_tokens <= kMaxTokens, IOS_E_ARG, "q_tokens out of range");
+    *bytes = split_bytes(q_tokens, d->heads, d->head_dim, tree_splits(*d, max_drafts));
+  });
+}
+
+extern "C" int ios_attn_tree(const ios_cache *c, int32_t layer, const ios_attn_desc *d, const ios_tokens *q,
+                             const ios_tokens *k, const ios_tokens *v, const ios_tokens *out, float *lse,
+                             const int32_t *seqs, const int32_t *cu, const int32_t *parent, int32_t max_drafts, void *work,
+                             int64_t work_bytes, void *hip_stream) {
+  return guarded([&] {
+    check_cache(c, true);
+    check_desc(d);
+    check_drafts(max_drafts);
+    check_tokens(q, d->dtype, "q");
+    check_tokens(k, d->dtype, "k");
+    check_tokens(v, d->dtype, "v");
+    check_out(out, d->dtype, d->heads, "out");
+    need(d->kv_heads == c->kv_heads && d->head_dim == c->head_dim, IOS_E_SHAPE, "the cache has other heads");
+    need(k->tokens == q->tokens && v->tokens == q->tokens && out->tokens == q->tokens, IOS_E_SHAPE,
+         "q, k, v and out must have the same rows");
+    need(seqs && cu && parent, IOS_E_ARG, "null list");
+    const CacheView cv = view(*c, layer);
+    if (q->tokens == 0) return;
+    need(q->tokens * d->heads <= INT32_MAX / 256 && (int64_t)max_drafts * d->heads <= 65535, IOS_E_UNSUPPORTED,
+         "too many rows and heads");
+    const int splits = usable(tree_splits(*d, max_drafts), q->tokens, *d, work, work_bytes);
+    launched(launch_attn_tree(cv, *d, *q, *k, *v, *out, lse, seqs, cu, parent, max_drafts, work, splits,
+                              (hipStream_t)hip_stream),
+             "ios_attn_tree");
+  });
+}
+
+extern "C" int ios_verify_work_bytes(const ios_verify_desc *d, int64_t *bytes) {
+  return guarded([&] {
+    check_verify(d);
+    need(bytes != nullptr, IOS_E_ARG, "null bytes");
+    *bytes = verify_bytes(*d);
+  });
+}
+
+extern "C" int ios_verify(const ios_verify_desc *d, const ios_rows *p, const ios_rows *q, const int32_t *tokens,
+                          const int32_t *parent, const int32_t *cu, const float *accept, const float *sample,
+                          int32_t *path, int32_t *count, int32_t *next, void *work, int64_t work_bytes,
+                          void *hip_stream) {
+  return guarded([&] {
+    check_verify(d);
+    check_rows(p, d, "p");
+    if (q) {
+      check_rows(q, d, "q");
+      need(q->rows == p->rows, IOS_E_SHAPE, "p and q have different lengths");
+    }
+    need(cu && path && count && next && sample, IOS_E_ARG, "null list");
+    need(p->rows == 0 || (tokens && parent && accept), IOS_E_ARG, "null list");
+    const int64_t size = verify_bytes(*d);
+    need(size == 0 || (work && aligned16(work) && work_bytes >= size), IOS_E_ARG,
+         "workspace below ios_verify_work_bytes or misaligned");
+    launched(launch_verify(*d, *p, q, tokens, parent, cu, accept, sample, path, count, next, work, (hipStream_t)hip_stream),
+             "ios_verify");
+  });
 }
 
 extern "C" int ios_cache_fork(const ios_cache *c, int32_t n, const int32_t *parents, const int32_t *children,
