@@ -379,7 +379,7 @@ extern "C" int ios_attn_tree_work_bytes(const ios_attn_desc *d, int64_t q_tokens
     check_drafts(max_drafts);
     need(bytes != nullptr, IOS_E_ARG, "null bytes");
     need(q_tokens >= 0 && q_tokens <= kMaxTokens, IOS_E_ARG, "q_tokens out of range");
-    *bytes = split_bytes(q_tokens, d->heads, d->head_dim, tree_splits(*d, max_drafts));
+    *bytes = tree_bytes(*d, q_tokens, max_drafts);
   });
 }
 
@@ -403,9 +403,9 @@ extern "C" int ios_attn_tree(const ios_cache *c, int32_t layer, const ios_attn_d
     if (q->tokens == 0) return;
     need(q->tokens * d->heads <= INT32_MAX / 256 && (int64_t)max_drafts * d->heads <= 65535, IOS_E_UNSUPPORTED,
          "too many rows and heads");
-    const int splits = usable(tree_splits(*d, max_drafts), q->tokens, *d, work, work_bytes);
-    launched(launch_attn_tree(cv, *d, *q, *k, *v, *out, lse, seqs, cu, parent, max_drafts, work, splits,
-                              (hipStream_t)hip_stream),
+    need(!work || (aligned16(work) && work_bytes >= tree_bytes(*d, q->tokens, max_drafts)), IOS_E_ARG,
+         "workspace below ios_attn_tree_work_bytes or misaligned");
+    launched(launch_attn_tree(cv, *d, *q, *k, *v, *out, lse, seqs, cu, parent, max_drafts, work, (hipStream_t)hip_stream),
              "ios_attn_tree");
   });
 }

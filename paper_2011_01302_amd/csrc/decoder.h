@@ -123,7 +123,7 @@ hipError_t launch_attn_cache(const CacheView &c, const ios_attn_desc &d, const i
                              float *lse, const int32_t *seqs, void *work, int splits, hipStream_t s);
 hipError_t launch_attn_tree(const CacheView &c, const ios_attn_desc &d, const ios_tokens &q, const ios_tokens &k,
                             const ios_tokens &v, const ios_tokens &out, float *lse, const int32_t *seqs,
-                            const int32_t *cu, const int32_t *parent, int most, void *work, int splits, hipStream_t s);
+                            const int32_t *cu, const int32_t *parent, int most, void *work, hipStream_t s);
 hipError_t launch_verify(const ios_verify_desc &d, const ios_rows &p, const ios_rows *q, const int32_t *tokens,
                          const int32_t *parent, const int32_t *cu, const float *accept, const float *sample,
                          int32_t *path, int32_t *count, int32_t *next, void *work, hipStream_t s);
@@ -141,8 +141,8 @@ hipError_t launch_copy(const ios_cache &c, int64_t page_bytes, int n, const int3
 // Over how many workgroups the keys of a row are spread (1: no workspace).
 int cache_splits(const ios_attn_desc &d);
 int prompt_splits(const ios_attn_desc &d, int64_t q_tokens);
-int tree_splits(const ios_attn_desc &d, int most);
-// Workspace of a check of drafts.
+// Workspace of attention of drafts, and of their check.
+int64_t tree_bytes(const ios_attn_desc &d, int64_t q_tokens, int most);
 int64_t verify_bytes(const ios_verify_desc &d);
 // Drafts of a sequence at most: a lane each, and a bit each in a mask.
 constexpr int kMaxDrafts = 64;
