@@ -18,7 +18,7 @@ constexpr int kWavesT = 8, kThreadsT = 64 * kWavesT;
 constexpr int kStagesT = 3;              // tiles of a wave's ring
 constexpr int kStepTiles = kWavesT;      // tiles of a step: one a wave
 // Steps that a block of rows costs beside its keys, the fewest of a share, and the keys from which blocks are cut.
-constexpr int kItemSteps = 3, kShareSteps = 4, kOneTree = 1024;
+constexpr int kItemSteps = 3, kShareSteps = 3, kOneTree = 1024;
 constexpr int64_t kRowsTree = 4096;       // rows from which a wave joins one: there are few parts of each
 
 // How the products over the cache are computed, for results in T:
@@ -213,10 +213,13 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
 
     // the queries as f16 operands, scaled by a power of two per row (as in single-token attention), and their sums by
     // group in three f16 parts, slot 4 kq + g of the product with a key's zero points: a wave for each 16 rows
-    const int my = wave % NB, row = min(r0 + 16 * my + col, rows - 1), draft = row / ratio;
-    const T *src = (const T *)q.data + (a + draft) * q.token_stride + (int64_t)(kvh * ratio + row - draft * ratio) * q.head_stride;
+    auto query = [&](int r) {
+      const int t = r / ratio;
+      return (const T *)q.data + (a + t) * q.token_stride + (int64_t)(kvh * ratio + r - t * ratio) * q.head_stride;
+    };
     auto q_at = [&](int n, int g, int p) { return (halfx8 *)(lds + RING) + ((n * G + g) * QP + p) * 64 + lane; };
     if (wave < NB) {
+      const T *src = query(min(r0 + 16 * wave + col, rows - 1));
       octet in[G];
       float top = 0.f;
 #pragma unroll
@@ -229,7 +232,7 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
       const int ex = __builtin_bit_cast(int, top) >> 23;          // biased exponent, 0 .. 255
       const int sh = ex == 0 || ex == 255 ? 0 : min(8 + 127 - ex, 126);
       float up = __builtin_bit_cast(float, (uint32_t)(127 + sh) << 23);
-      if (kq == 0) mul_of[16 * my + col] = fmaxf(__builtin_fabsf(scale) * kLog2e / up, 1e-30f);
+      if (kq == 0) mul_of[16 * wave + col] = fmaxf(__builtin_fabsf(scale) * kLog2e / up, 1e-30f);
       up = scale < 0.f ? -up : up;
       halfx4 z = {0, 0, 0, 0};
 #pragma unroll
@@ -247,14 +250,14 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
           }
         }
 #pragma unroll
-        for (int p = 0; p < QP; ++p) *q_at(my, g, p) = parts[p];
+        for (int p = 0; p < QP; ++p) *q_at(wave, g, p) = parts[p];
         if constexpr (!kHeldKeys<T>) {
           s = col_sum(s);
           const _Float16 hi = (_Float16)s, lo = (_Float16)(s - (float)hi);
           z[g] = kq == 0 ? hi : kq == 1 ? lo : kq == 2 ? (_Float16)(s - (float)hi - (float)lo) : (_Float16)0;
         }
       }
-      if constexpr (!kHeldKeys<T>) sums_of[my][lane] = z;
+      if constexpr (!kHeldKeys<T>) sums_of[wave][lane] = z;
     }
     float mx_[NB], l[NB];                                           // reference and sum of a row's weights
     floatx4 o[NB][NT];
@@ -268,12 +271,14 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
       for (int t = 0; t < NT; ++t) o[n][t] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // the drafts' own keys, a tile of them and a block of rows for each wave of the first range; every load first
-    const int k0 = wave / NB * kTileKeys;
+    // the drafts' own keys, a tile of them and 16 rows for each wave, from the last wave on; every load first
+    const int my = (kWavesT - 1 - wave) % NB, k0 = (kWavesT - 1 - wave) / NB * kTileKeys;
     if (from == 0 && k0 < m && r0 + 16 * my < rows) {
       const T *kd = (const T *)k.data + a * k.token_stride + kvh * k.head_stride;
       const T *vd = (const T *)v.data + a * v.token_stride + kvh * v.head_stride;
       const int keys = min(m - k0, kTileKeys);
+      const int row = min(r0 + 16 * my + col, rows - 1), draft = row / ratio;
+      const T *src = query(row);
       T val[NT][8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -727,10 +732,22 @@ __global__ __launch_bounds__(256) void attn_tree_join_kernel(int heads, int rati
 
 int64_t keys_of(const ios_attn_desc &d) { return d.max_keys ? d.max_keys : 1 << 16; }
 
-// Blocks of 16 rows that a workgroup takes.
-int row_blocks(const ios_attn_desc &d, int most) {
+// Steps of the whole call at most, with blocks of w rows: no more blocks have rows than every sequence's most, nor than all
+// rows make.
+int64_t steps_of(const ios_attn_desc &d, int64_t q_tokens, int most, int w) {
+  const int ratio = d.heads / d.kv_heads;
+  const int64_t blocks = std::min<int64_t>((int64_t)d.seqs * ((most * ratio + w - 1) / w), q_tokens * ratio / w + d.seqs);
+  return d.kv_heads * blocks * (kItemSteps + (keys_of(d) + kStepTiles * kTileKeys - 1) / (kStepTiles * kTileKeys));
+}
+
+// 16-row groups of a block.  Four read the cache once for 64 rows, but each wave then begins and ends with twice the work of
+// two: 32 sequences under 64 rows each 285 us against 371 (bf16; f16 532 against 574), one under 256 rows 77 against 83, but
+// maps of 1 to 3100 tokens 36 against 31 (f16 44 against 37).  So four where every workgroup has 12 steps; float32's three
+// parts of the queries and weights leave registers for two.
+int row_groups(const ios_attn_desc &d, int64_t q_tokens, int most) {
   const int rows = most * (d.heads / d.kv_heads);
-  return rows <= 16 ? 1 : rows <= 32 || d.dtype == IOS_F32 ? 2 : 4;
+  if (rows <= 16) return 1;
+  return rows <= 32 || d.dtype == IOS_F32 || steps_of(d, q_tokens, most, 64) < 12 * 256 ? 2 : 4;
 }
 
 struct Call {
@@ -766,7 +783,7 @@ hipError_t run(const Call &x) {
 
 template <class T, int G>
 hipError_t for_blocks(const Call &x) {
-  switch (row_blocks(*x.d, x.most)) {
+  switch (row_groups(*x.d, x.q.tokens, x.most)) {
     case 1: return run<T, G, 1>(x);
     case 2: return run<T, G, 2>(x);
     default:
@@ -788,10 +805,7 @@ hipError_t for_groups(const Call &x) {
 // Workgroups that share the keys (0: each takes a block of rows with all of its keys).
 int groups_of(const ios_attn_desc &d, int64_t q_tokens, int most) {
   if (keys_of(d) < kOneTree) return 0;
-  const int ratio = d.heads / d.kv_heads, w = 16 * row_blocks(d, most);
-  // blocks that have rows: no more than every sequence's most, nor than all rows make
-  const int64_t blocks = d.kv_heads * std::min<int64_t>((int64_t)d.seqs * ((most * ratio + w - 1) / w), q_tokens * ratio / w + d.seqs);
-  const int64_t steps = blocks * (kItemSteps + (keys_of(d) + kStepTiles * kTileKeys - 1) / (kStepTiles * kTileKeys));
+  const int64_t steps = steps_of(d, q_tokens, most, 16 * row_groups(d, q_tokens, most));
   const int card = 256 * (d.head_dim <= 64 ? 2 : 1);              // that the card's LDS holds at a time
   return (int)std::min<int64_t>(card, (steps + kShareSteps - 1) / kShareSteps);
 }
@@ -799,7 +813,7 @@ int groups_of(const ios_attn_desc &d, int64_t q_tokens, int most) {
 }  // namespace
 
 int64_t tree_bytes(const ios_attn_desc &d, int64_t q_tokens, int most) {
-  const int64_t groups = groups_of(d, q_tokens, most), w = 16 * row_blocks(d, most);
+  const int64_t groups = groups_of(d, q_tokens, most), w = 16 * row_groups(d, q_tokens, most);
   return groups ? 2 * groups * w * (d.head_dim + 2) * (int64_t)sizeof(float) + q_tokens * d.heads * (int64_t)sizeof(PartRef) : 0;
 }
 
