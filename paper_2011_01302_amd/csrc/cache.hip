@@ -129,39 +129,58 @@ template <> struct Source<KEPT> {
   const int32_t *count;
   int most;
 };
-constexpr int kQueryHeads = 4;          // heads of queries that a workgroup turns
+constexpr int kQueryHeads = 8;          // heads of queries that a workgroup turns
+
+// Cosines and sines of a tile's tokens, [token][pair].
+__device__ __forceinline__ void turns_of(const ios_rotary &r, const TileJob &j, int half, float2 *cs) {
+  for (int y = threadIdx.x; y < (j.hi - j.lo) * half; y += 256)
+    cs[y] = turn_of(j.pos + j.lo + y / half, r.freq[y % half], r.amplitude);
+}
 
 // The queries of a tile's tokens, up to kQueryHeads heads from head0 on.
 template <class T>
-__device__ __forceinline__ void turn_queries(const Source<TURNED> &x, const TileJob &j, int dim, int head0) {
-  __shared__ float2 cs[kTileKeys * kMaxPairs];
+__device__ __forceinline__ void turn_queries(const Source<TURNED> &x, const TileJob &j, int dim, int head0, float2 *cs) {
+  constexpr int N = 4;                                       // units on their way at once
   const RotaryUnits u(x.r, dim);
-  const int heads = min(x.heads - head0, kQueryHeads), keys = j.hi - j.lo;
-  for (int y = threadIdx.x; y < keys * u.half; y += 256)
-    cs[y] = turn_of(j.pos + j.lo + y / u.half, x.r.freq[y % u.half], x.r.amplitude);
+  const int heads = min(x.heads - head0, kQueryHeads), units = (j.hi - j.lo) * heads * u.all;
+  RotaryUnit<T> unit[N];
+  int at[N], key[N], head[N];
+  auto row = [&](const ios_tokens &a, int e) {
+    return (T *)a.data + (j.row + j.lo + key[e]) * a.token_stride + (head0 + head[e]) * a.head_stride;
+  };
+  auto load = [&](int y0) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int y = min(y0 + 256 * e, units - 1), z = y / u.all;
+      at[e] = y - z * u.all;
+      key[e] = z / heads;
+      head[e] = z - key[e] * heads;
+      unit[e].load(u, row(x.q, e), at[e]);
+    }
+  };
+  load(threadIdx.x);
+  turns_of(x.r, j, u.half, cs);
   __syncthreads();
-  for (int y = threadIdx.x; y < keys * heads * u.all; y += 256) {
-    const int row = y / u.all, at = y - row * u.all, key = row / heads, h = head0 + row - key * heads;
-    const int64_t t = j.row + j.lo + key;
-    RotaryUnit<T> unit;
-    unit.load(u, (const T *)x.q.data + t * x.q.token_stride + h * x.q.head_stride, at);
-    unit.turn_by(u, cs + key * u.half, at);
-    unit.store(u, (T *)x.qo.data + t * x.qo.token_stride + h * x.qo.head_stride, at);
+  for (int y0 = threadIdx.x; y0 < units; y0 += 256 * N) {
+    if (y0 != (int)threadIdx.x) load(y0);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (y0 + 256 * e < units) {
+        unit[e].turn_by(u, cs + key[e] * u.half, at[e]);
+        unit[e].store(u, row(x.qo, e), at[e]);
+      }
   }
 }
 
 // The tile's keys, octet tid + 256 u of them in kr[u].
 template <class T, int G, int N>
-__device__ __forceinline__ void turn_keys(const ios_rotary &r, const TileJob &j, Row8<T> (&kr)[N]) {
-  __shared__ __align__(16) T rows[kTileKeys * 32 * G];
-  __shared__ float2 cs[kTileKeys * kMaxPairs];
+__device__ __forceinline__ void turn_keys(const ios_rotary &r, const TileJob &j, Row8<T> (&kr)[N], T *rows, float2 *cs) {
   const RotaryUnits u(r, 32 * G);
   const int tid = threadIdx.x, keys = j.hi - j.lo;
+  turns_of(r, j, u.half, cs);
 #pragma unroll
   for (int e = 0; e < N; ++e)
     if (tid + 256 * e < kTileKeys * 4 * G) *(Row8<T> *)(rows + (tid + 256 * e) * 8) = kr[e];
-  for (int y = tid; y < keys * u.half; y += 256)
-    cs[y] = turn_of(j.pos + j.lo + y / u.half, r.freq[y % u.half], r.amplitude);
   __syncthreads();
   for (int y = tid; y < keys * u.turned; y += 256) {
     const int key = y / u.turned, at = y - key * u.turned;
@@ -183,6 +202,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, ios_toke
                                                            const int32_t *seqs, const int32_t *cu, Source<M> from) {
   __shared__ uint32_t img[tile_bytes(G) / 4];
   __shared__ uint32_t vc[kTileKeys * 4 * G];                 // codes of V by key and octet of values
+  __shared__ __align__(16) T turned[M == TURNED ? kTileKeys * 32 * G : 1];
+  __shared__ float2 cs[M == TURNED ? kTileKeys * 16 * G : 1];
   const int tid = threadIdx.x, head = blockIdx.y;
   int seq;
   TileJob j;
@@ -191,7 +212,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, ios_toke
   if ((!j.tile && !(M == TURNED && head >= c.heads)) || j.lo >= j.hi) return;
   if constexpr (M == TURNED) {
     if (head >= c.heads) {
-      turn_queries<T>(from, j, 32 * G, (head - c.heads) * kQueryHeads);
+      turn_queries<T>(from, j, 32 * G, (head - c.heads) * kQueryHeads, cs);
       return;
     }
   }
@@ -210,7 +231,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, ios_toke
     kr[u] = *(const Row8<T> *)((const T *)k.data + row * k.token_stride + head * k.head_stride + oct * 8);
     vr[u] = *(const Row8<T> *)((const T *)v.data + row * v.token_stride + head * v.head_stride + oct * 8);
   }
-  if constexpr (M == TURNED) turn_keys<T, G, N>(from.r, j, kr);
+  if constexpr (M == TURNED) turn_keys<T, G, N>(from.r, j, kr, turned, cs);
   uintx4 *gt = (uintx4 *)j.tile, *li = (uintx4 *)img;
   for (int i = tid; i < tile_bytes(G) / 16; i += 256) li[i] = j.lo > 0 ? gt[i] : uintx4{0, 0, 0, 0};
   __syncthreads();

@@ -11,33 +11,37 @@ namespace {
 
 constexpr int kUnroll = 4;               // units of a thread on their way at once
 
+// x / d by a product with ceil(2^32 / d), right where x d < 2^32.
+struct Divisor {
+  uint32_t d, m;
+  explicit Divisor(uint32_t d) : d(d), m((uint32_t)((((uint64_t)1 << 32) + d - 1) / d)) {}
+  __device__ __forceinline__ int of(int x) const { return d == 1 ? x : (int)__umulhi((uint32_t)x, m); }
+};
+
 template <class T>
-__global__ __launch_bounds__(256) void rotate_kernel(ios_rotary r, int head_dim, int per, ios_tokens q, ios_tokens qo,
-                                                     int heads, ios_tokens k, ios_tokens ko, int kv_heads,
+__global__ __launch_bounds__(256) void rotate_kernel(ios_rotary r, int head_dim, int per, Divisor by_unit, Divisor by_head,
+                                                     ios_tokens q, ios_tokens qo, int heads, ios_tokens k, ios_tokens ko,
                                                      const int32_t *pos) {
   extern __shared__ float2 table[];      // [per][half]
   const RotaryUnits u(r, head_dim);
   const int64_t t0 = (int64_t)blockIdx.x * per;
-  const int tokens = (int)min((int64_t)per, q.tokens - t0), all = heads + kv_heads;
-  // heads of this workgroup
-  const int h0 = (int)((int64_t)all * blockIdx.y / gridDim.y), h1 = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y);
-  const int units = tokens * (h1 - h0) * u.all;
-  auto place = [&](int x, int *at, int *t, const ios_tokens &a, const ios_tokens &b) {
-    const int row = x / u.all, tok = row / (h1 - h0), h = h0 + row - tok * (h1 - h0);
-    *at = x - row * u.all;
-    *t = tok;
-    return h < heads ? (T *)a.data + (t0 + tok) * a.token_stride + h * a.head_stride
-                     : (T *)b.data + (t0 + tok) * b.token_stride + (h - heads) * b.head_stride;
-  };
+  const int tokens = (int)min((int64_t)per, q.tokens - t0), all = by_head.d, units = tokens * all * u.all;
   RotaryUnit<T> unit[kUnroll];
-  int at, t;
+  int at[kUnroll], tok[kUnroll], head[kUnroll];
+  auto row = [&](int e, const ios_tokens &a, const ios_tokens &b) {
+    const bool is_k = head[e] >= heads;
+    const int64_t ts = is_k ? b.token_stride : a.token_stride, hs = is_k ? b.head_stride : a.head_stride;
+    return (T *)(is_k ? b.data : a.data) + (t0 + tok[e]) * ts + (head[e] - (is_k ? heads : 0)) * hs;
+  };
   auto load = [&](int x0) {
 #pragma unroll
-    for (int e = 0; e < kUnroll; ++e)
-      if (x0 + 256 * e < units) {
-        const T *row = place(x0 + 256 * e, &at, &t, q, k);
-        unit[e].load(u, row, at);
-      }
+    for (int e = 0; e < kUnroll; ++e) {
+      const int x = min(x0 + 256 * e, units - 1), y = by_unit.of(x);
+      at[e] = x - y * u.all;
+      tok[e] = by_head.of(y);
+      head[e] = y - tok[e] * all;
+      unit[e].load(u, row(e, q, k), at[e]);
+    }
   };
   load(threadIdx.x);
   for (int x = threadIdx.x; x < tokens * u.half; x += 256)
@@ -48,9 +52,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(ios_rotary r, int head_dim,
 #pragma unroll
     for (int e = 0; e < kUnroll; ++e)
       if (x0 + 256 * e < units) {
-        T *row = place(x0 + 256 * e, &at, &t, qo, ko);
-        unit[e].turn_by(u, table + t * u.half, at);
-        unit[e].store(u, row, at);
+        unit[e].turn_by(u, table + tok[e] * u.half, at[e]);
+        unit[e].store(u, row(e, qo, ko), at[e]);
       }
   }
 }
@@ -58,11 +61,11 @@ __global__ __launch_bounds__(256) void rotate_kernel(ios_rotary r, int head_dim,
 template <class T>
 hipError_t run(const ios_rotary &r, int head_dim, const ios_tokens &q, const ios_tokens &qo, int heads,
                const ios_tokens &k, const ios_tokens &ko, int kv_heads, const int32_t *pos, hipStream_t s) {
-  const int per = q.tokens >= 2048 ? 4 : 1;
-  const int64_t blocks = (q.tokens + per - 1) / per;
-  const int groups = 1;
-  hipLaunchKernelGGL((rotate_kernel<T>), dim3((unsigned)blocks, groups), dim3(256), per * (r.dim / 2) * sizeof(float2), s, r,
-                     head_dim, per, q, qo, heads, k, ko, kv_heads, pos);
+  // tokens of a workgroup: up to kUnroll units a thread, but every CU has four workgroups first
+  const RotaryUnits u(r, head_dim);
+  const int all = heads + kv_heads, per = (int)std::max<int64_t>(1, std::min<int64_t>(256 * kUnroll / (all * u.all), q.tokens / 1024));
+  hipLaunchKernelGGL((rotate_kernel<T>), dim3((unsigned)((q.tokens + per - 1) / per)), dim3(256),
+                     per * u.half * sizeof(float2), s, r, head_dim, per, Divisor(u.all), Divisor(all), q, qo, heads, k, ko, pos);
   return hipGetLastError();
 }
 

@@ -16,7 +16,7 @@ namespace ios {
 
 namespace {
 
-constexpr int kThreadsV = 1024, kWavesV = kThreadsV / 64, kStep = kThreadsV * 8, kUnrollV = 4;
+constexpr int kThreadsV = 1024, kThreadsD = 512, kUnrollV = 4;   // of a walk, and of a share of a row
 constexpr int kMaxShares = 64;
 
 // Where a walk stopped.
@@ -65,14 +65,17 @@ __device__ __forceinline__ Raw8<T> raw8(const T *row, int64_t t, int64_t end) {
 }
 
 // What the threads of a workgroup tell each other; two of each, so that one can be written while the other is read.
+template <int TH>
 struct Scratch {
-  double sums[2][kWavesV];
-  int32_t hit[2][kWavesV], heavy[2][kWavesV];
+  static constexpr int kWaves = TH / 64;
+  double sums[2][kWaves];
+  int32_t hit[2][kWaves], heavy[2][kWaves];
 };
 
-// What is left of a row: max(p - c q, 0), or p without some tokens.
-template <class T, bool GIVEN>
+// What is left of a row: max(p - c q, 0), or p without some tokens.  For a workgroup of TH threads.
+template <class T, bool GIVEN, int TH>
 struct Rest {
+  static constexpr int kWaves = TH / 64, kStep = TH * 8;
   const T *p, *q;
   double c;
   const int32_t *out;
@@ -124,13 +127,13 @@ struct Rest {
     __syncthreads();
     s = 0.0;
 #pragma unroll
-    for (int w = 0; w < kWavesV; ++w) s += sums[w];
+    for (int w = 0; w < kWaves; ++w) s += sums[w];
     return uniform(s);
   }
 
   // The first token of from .. end - 1 with any weight whose running sum, `before` ahead of them, passes the mark; where
   // none does (a mark at the very end), the last with any weight.  In every thread.
-  __device__ __forceinline__ int32_t find(int64_t from, int64_t end, double before, double mark, Scratch &lds) const {
+  __device__ __forceinline__ int32_t find(int64_t from, int64_t end, double before, double mark, Scratch<TH> &lds) const {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int turn = 0, last = -1;
     for (int64_t t1 = from; t1 < end; t1 += kStep, turn ^= 1) {
@@ -153,7 +156,7 @@ struct Rest {
       __syncthreads();
       double run = before + (incl - s);
 #pragma unroll
-      for (int x = 0; x < kWavesV; ++x) {
+      for (int x = 0; x < kWaves; ++x) {
         run += x < wave ? lds.sums[turn][x] : 0.0;
         before += lds.sums[turn][x];
       }
@@ -172,7 +175,7 @@ struct Rest {
       if (lane == 0) lds.hit[turn][wave] = hit, lds.heavy[turn][wave] = heavy;
       __syncthreads();
 #pragma unroll
-      for (int x = 0; x < kWavesV; ++x) {
+      for (int x = 0; x < kWaves; ++x) {
         hit = min(hit, lds.hit[turn][x]);
         last = max(last, lds.heavy[turn][x]);
       }
@@ -183,12 +186,12 @@ struct Rest {
   }
 };
 
-// The next token of a row: its shares' sums are known, `share` tokens each.
-template <class T, bool GIVEN>
-__device__ __forceinline__ int32_t pick(Rest<T, GIVEN> rest, int64_t vocab, int64_t share, int shares, const double *sums,
-                                        float sample, Scratch &lds) {
+// The next token of a row: the sum of its share x is lane x's, `share` tokens each.
+template <class T, bool GIVEN, int TH>
+__device__ __forceinline__ int32_t pick(Rest<T, GIVEN, TH> rest, int64_t vocab, int64_t share, int shares, double sums,
+                                        float sample, Scratch<TH> &lds) {
   double whole = 0.0;
-  for (int x = 0; x < shares; ++x) whole += sums[x];
+  for (int x = 0; x < shares; ++x) whole += of_lane(sums, x);
   double mark = fmax((double)sample, 0.0) * whole, before = 0.0;
   int64_t from = 0, end = vocab;
   if (!uniform(whole > 0.0)) {                                    // nothing is left: from p itself
@@ -201,9 +204,9 @@ __device__ __forceinline__ int32_t pick(Rest<T, GIVEN> rest, int64_t vocab, int6
     int at = -1, last = 0;
     double upto = 0.0;
     for (int x = 0; x < shares; ++x) {
-      const double s = sums[x];
-      if (at < 0 && upto + s > mark) at = x, before = upto;
-      if (s > 0.0) last = x;
+      const double s = of_lane(sums, x);
+      if (at < 0 && uniform(upto + s > mark)) at = x, before = upto;
+      if (uniform(s > 0.0)) last = x;
       upto += s;
     }
     if (at < 0) at = last, mark = INFINITY;
@@ -219,8 +222,7 @@ __global__ __launch_bounds__(kThreadsV) void verify_kernel(int vocab, int most, 
                                                            const int32_t *tokens, const int32_t *parent,
                                                            const int32_t *cu, const float *accept, const float *sample,
                                                            int32_t *path, int32_t *count, int32_t *next, Stop *stop) {
-  __shared__ Scratch lds;
-  __shared__ double whole[1];
+  __shared__ Scratch<kThreadsV> lds;
   __shared__ int32_t left_out[kMaxDrafts];
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t a = clip(cu[i], p.rows), b = clip(cu[i + 1], p.rows);
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(kThreadsV) void verify_kernel(int vocab, int most, 
   bool summed = false;                                            // left_sum is what is left of the node's row
   auto rest = [&](int out_n) {
     const int64_t row = a + node;
-    return Rest<T, GIVEN>{(const T *)p.data + row * p.row_stride, (const T *)q.data + row * q.row_stride, C, left_out, out_n};
+    return Rest<T, GIVEN, kThreadsV>{(const T *)p.data + row * p.row_stride, (const T *)q.data + row * q.row_stride, C, left_out, out_n};
   };
   uint64_t gone = 0, children = __ballot(sound && up == 0);
   while (children) {
@@ -301,22 +303,19 @@ __global__ __launch_bounds__(kThreadsV) void verify_kernel(int vocab, int most, 
   }
   if (!ONE) return;
   __syncthreads();                                                // left_out
-  const Rest<T, GIVEN> r = rest(out_n);
+  const Rest<T, GIVEN, kThreadsV> r = rest(out_n);
   if (!summed) {
     left_sum = r.sum(0, vocab, lds.sums[turn]);
     __syncthreads();
   }
-  if (tid == 0) whole[0] = left_sum;
-  __syncthreads();
-  const int32_t t = pick(r, (int64_t)vocab, (int64_t)vocab, 1, whole, sample[i], lds);
+  const int32_t t = pick(r, (int64_t)vocab, (int64_t)vocab, 1, left_sum, sample[i], lds);
   if (tid == 0) next[i] = t;
 }
 
 template <class T, bool GIVEN>
-__global__ __launch_bounds__(kThreadsV) void verify_draw_kernel(int vocab, int share, ios_rows p, ios_rows q,
+__global__ __launch_bounds__(kThreadsD) void verify_draw_kernel(int vocab, int share, ios_rows p, ios_rows q,
                                                                 const float *sample, int32_t *next, Stop *stop) {
-  __shared__ Scratch lds;
-  __shared__ double parts[kMaxShares];
+  __shared__ Scratch<kThreadsD> lds;
   __shared__ int32_t left_out[kMaxDrafts], last;
   const int i = blockIdx.y, tid = threadIdx.x, shares = gridDim.x;
   Stop &st = stop[i];
@@ -325,26 +324,29 @@ __global__ __launch_bounds__(kThreadsV) void verify_draw_kernel(int vocab, int s
   const int out_n = GIVEN ? 0 : st.out_n;
   if (tid < out_n) left_out[tid] = st.out[tid];
   __syncthreads();
-  const Rest<T, GIVEN> r{(const T *)p.data + row * p.row_stride, (const T *)q.data + row * q.row_stride, st.c, left_out, out_n};
+  const Rest<T, GIVEN, kThreadsD> r{(const T *)p.data + row * p.row_stride, (const T *)q.data + row * q.row_stride, st.c, left_out, out_n};
   const int64_t from = (int64_t)blockIdx.x * share;
   const double s = r.sum(from, min(from + share, (int64_t)vocab), lds.sums[0]);
-  if (tid == 0) {                                                 // the share's sum before the count, for the whole device
-    __hip_atomic_store(&st.sums[blockIdx.x], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(&st.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
+  if (tid == 0) {
+    // the sum before the count, and no more than that: an exchange has happened for the whole device once its old value is
+    // back (a release would write back all that the L2s hold, for every share)
+    const double old = __hip_atomic_exchange(&st.sums[blockIdx.x], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::"v"(old) : "memory");
+    last = __hip_atomic_fetch_add(&st.done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
   }
   __syncthreads();
   if (!last) return;
-  if (tid < shares) parts[tid] = __hip_atomic_load(&st.sums[tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  const int32_t t = pick(r, (int64_t)vocab, (int64_t)share, shares, parts, sample[i], lds);
+  static_assert(kMaxShares <= 64, "a lane for each share");
+  const double sums = __hip_atomic_load(&st.sums[min(tid & 63, shares - 1)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const int32_t t = pick(r, (int64_t)vocab, (int64_t)share, shares, sums, sample[i], lds);
   if (tid == 0) next[i] = t;
 }
 
 // Workgroups that sum a row: one (and no second launch) for a small vocabulary.
 int shares_of(const ios_verify_desc &d) {
-  if (d.vocab < 2 * kStep) return 1;
-  const int64_t want = (512 + d.seqs - 1) / d.seqs;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMaxShares), d.vocab / kStep));
+  if (d.vocab < 2 * kThreadsV * 8) return 1;
+  const int64_t want = (2048 + d.seqs - 1) / d.seqs;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMaxShares), d.vocab / (kThreadsD * 8)));
 }
 
 }  // namespace
@@ -371,7 +373,7 @@ hipError_t launch_verify(const ios_verify_desc &d, const ios_rows &p, const ios_
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int share = ((d.vocab + shares - 1) / shares + 7) / 8 * 8;
-    hipLaunchKernelGGL((verify_draw_kernel<T, GIVEN>), dim3(shares, d.seqs), dim3(kThreadsV), 0, s, d.vocab, share, p, qq,
+    hipLaunchKernelGGL((verify_draw_kernel<T, GIVEN>), dim3(shares, d.seqs), dim3(kThreadsD), 0, s, d.vocab, share, p, qq,
                        sample, next, stop);
     return hipGetLastError();
   };
