@@ -802,12 +802,11 @@ hipError_t for_groups(const Call &x) {
   }
 }
 
-// Workgroups that share the keys (0: each takes a block of rows with all of its keys).
+// Workgroups that share the keys, one a CU at most (0: each takes a block of rows with all of its keys).
 int groups_of(const ios_attn_desc &d, int64_t q_tokens, int most) {
   if (keys_of(d) < kOneTree) return 0;
   const int64_t steps = steps_of(d, q_tokens, most, 16 * row_groups(d, q_tokens, most));
-  const int card = 256 * (d.head_dim <= 64 ? 2 : 1);              // that the card's LDS holds at a time
-  return (int)std::min<int64_t>(card, (steps + kShareSteps - 1) / kShareSteps);
+  return (int)std::min<int64_t>(256, (steps + kShareSteps - 1) / kShareSteps);
 }
 
 }  // namespace
