@@ -340,7 +340,9 @@ def tree_reference(typ, q, kc, vc, kd, vd, see, scale):
     ac, ad = pc @ (vz.abs() + 15 * vs), pd @ v0.abs()
     ps, a = pc @ vs, ac + ad
     top = float((vz + vs * vcode).abs().max()) if m else 0.0
-    w, summed = {"bf16": (2.0 ** -10 * ac + 2.0 ** -38 * m * top, a), "f16": (2.0 ** -16 * 143 * ps, pc @ (vz.abs() + 271 * vs) + ad),
+    # bf16: weights are 2^9 at least where a row's largest score is, in f16, so off by half a step of 2^-11 or by 2^-25 at
+    # most: 2^-34 of the largest weight for each key, and that is at most the sum of them
+    w, summed = {"bf16": (2.0 ** -10 * ac + 2.0 ** -34 * m * top, a), "f16": (2.0 ** -16 * 143 * ps, pc @ (vz.abs() + 271 * vs) + ad),
                  "f32": (2.0 ** -24 * 15 * ps, a)}[typ]
     r = 33 * -(-m // 128) + 128 + 8 + 40 + 128
     fine = torch.where(torch.isfinite(out), out, 0.0).abs()
@@ -513,6 +515,51 @@ def test_tree_largest_values_stay_finite(typ):
             assert torch.isfinite(out[:, h]).all() and (err <= bound).all(), float((err / bound).max())
 
 
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("size,low", [(8.0, -110.0), (1.0, -200.0)])
+def test_tree_large_value_of_no_weight(typ, size, low):
+    """A value of 2^100 whose weight is e^-110 or less leaves the other keys' weights as exact as they were; one of 2^120 with
+    a score of -20 is what its row comes to: cached scores, size times a normal number and a small one, stay below 45, so its
+    weight is e^-65 / 2500 = 2^-106 at least."""
+    dt = TYPES[typ][0]
+    c, hk, hv = cached(1, 64, 64, [2500], 23)
+    u = torch.zeros(64, device=DEV)
+    u[5] = size
+    q = (randn((6, 4, 64), torch.float32, 1, 0.125) + u).to(dt)
+    k, v = randn((6, 1, 64), dt, 2, 0.25), randn((6, 1, 64), dt, 3)
+    k[1, 0], v[1, 0, 7] = (low / size * u / size).to(dt), 2.0 ** 100
+    k[4, 0], v[4, 0, 9] = (-20.0 / size * u / size).to(dt), -2.0 ** 120
+    parents = [[-1, 0, 1, 1, 0, 4]]
+    out = check_tree(typ, c, q, k, v, [0], [6], parents, hk, hv, max_keys=2500, scale=1.0)
+    assert (out[1:4].abs() < 100).all() and (out[4:, :, 9] < -2.0 ** 13).all()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f16"])
+@pytest.mark.parametrize("bound", [5000, 0])
+def test_tree_ragged_batch(typ, bound):
+    """Shares that begin and end inside blocks of rows and sequences, with trees of every size: 64 rows a block where the
+    lengths may be long, 32 where they may not."""
+    rng = np.random.default_rng(3)
+    lens = [int(x) for x in np.exp(rng.uniform(0, math.log(5000), 18))] + [0, 5000]
+    drafts = [int(x) for x in rng.integers(0, 33, 20)]
+    c, hk, hv = cached(2, 64, 32, lens, 29)
+    parents, n = [forest(m, rng, "tree") for m in drafts], sum(drafts)
+    dt = TYPES[typ][0]
+    q, k, v = randn((n, 6, 64), dt, 5), randn((n, 2, 64), dt, 6), randn((n, 2, 64), dt, 7)
+    order = [int(x) for x in rng.permutation(20)]
+    check_tree(typ, c, q, k, v, order, drafts, parents, hk, hv, max_keys=bound)
+
+
+def test_tree_more_sequences_than_threads():
+    """1300 sequences, three for a thread that lays out the shares, some listed twice, some without drafts or tokens."""
+    lens = [(37 * i) % 120 for i in range(40)]
+    c, hk, hv = cached(1, 32, 32, lens, 31)
+    drafts = [(i * i) % 4 for i in range(1300)]
+    parents, n = [[j - 1 for j in range(m)] for m in drafts], sum(drafts)
+    q, k, v = randn((n, 1, 32), torch.float16, 1), randn((n, 1, 32), torch.float16, 2), randn((n, 1, 32), torch.float16, 3)
+    check_tree("f16", c, q, k, v, [(7 * i) % 43 - 1 for i in range(1300)], drafts, parents, hk, hv)
+
+
 @ALL
 @pytest.mark.parametrize("lead", [11.5, 18.0])
 def test_tree_long_tail(typ, lead):
@@ -566,6 +613,42 @@ def test_tree_bad_offsets_and_many_sequences():
     assert (out[:13] == 7).all() and (out[13:16] != 7).any() and (out[80 + 13:] == 7).all()
     out, _, _ = tree("f16", c, q, k, v, [1, 2], [50, 20, 10], flat, 64)
     assert (out == 7).all()
+
+
+def test_tree_in_a_graph_with_other_lengths():
+    """One recorded call, replayed with other cached lengths, trees and lists: the shares are laid out anew each time."""
+    lens = [4000, 1, 900, 2600]
+    c, hk, hv = cached(2, 64, 32, lens, 37)
+    rng = np.random.default_rng(5)
+    n, most, dt = 96, 32, torch.float16
+    q, k, v = randn((n, 8, 64), dt, 5), randn((n, 2, 64), dt, 6), randn((n, 2, 64), dt, 7)
+    d = desc("f16", 8, 2, 64, 3, 0, 4000)
+    size = I.ios_attn_tree_work_bytes(d, n, most)
+    work = [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    out, again = torch.zeros_like(q), torch.zeros_like(q)
+    seqs, cu, parent = i32([0, 1, 2]), i32([0, 0, 0, 0]), i32([-1] * n)
+
+    def call(o, w):
+        I.ios_attn_tree(c.c, 0, d, toks(q), toks(k), toks(v), toks(o), 0, seqs.data_ptr(), cu.data_ptr(), parent.data_ptr(),
+                        most, w.data_ptr(), size, stream())
+    call(out, work[0])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(out, work[0])
+    for i in range(8):
+        drafts = [int(x) for x in rng.integers(0, 33, 3)]
+        order = [int(x) for x in rng.permutation(4)[:3]]
+        parents = [forest(m, rng, "tree") for m in drafts]
+        flat = [p for t in parents for p in t]
+        seqs.copy_(i32(order)), cu.copy_(i32(offsets(drafts))), parent.copy_(i32(flat + [-1] * (n - len(flat))))
+        out.fill_(7.0), again.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        call(again, work[1])
+        torch.cuda.synchronize()
+        assert torch.equal(out, again) and (out[sum(drafts):] == 7).all(), i
+        check_tree("f16", c, q, k, v, order, drafts, parents, hk, hv, max_keys=4000)
 
 
 # ---------------------------------------------------------------- the check of drafts
