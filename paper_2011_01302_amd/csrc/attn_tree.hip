@@ -25,14 +25,18 @@ constexpr int64_t kRowsTree = 4096;       // rows from which a wave joins one: t
 // bf16: keys and values z + s c rounded to f16 (2^-11 at most, against 2^-8 of the result), weights to f16
 // f16: scores z sum(q) + s (c . q) with exact codes; values and weights in two f16 parts each, of whose products the one of
 //      both second parts is left out (2^-22)
-// f32: the same scores with q in three f16 parts; p s in three bf16 parts times exact codes, zero points in 32 bits
+// f32: the same scores with q in three f16 parts; p s in three bf16 parts times exact codes, zero points in 32 bits.  Codes
+//      are taken from 8 on, (z + 8 s) + s (c - 8), so that no term is much larger than the value (with the zero point at the
+//      least value results were 1.2e-6 of their size off over 785 tokens, elementary operations in float32 5e-7)
 template <class T> constexpr bool kHeldKeys = std::is_same_v<T, __bf16>;
 template <class T> constexpr int kQueryParts = std::is_same_v<T, float> ? 3 : 1;
 
-// The largest weight is 2^kTopTree when its row's reference is set, and the reference is set anew when one would pass
-// 2^kFarTree: rows whose largest score grows by less than 6 (base 2) from the first tile on, which are nearly all, keep the
-// first.  A 16-bit weight is off by at most 2^-25, so 2^-34 of the largest: 10^6 keys together by 2^-14.
-constexpr float kTopTree = 9.f, kFarTree = 15.f;
+// The largest weight is 2^kTopTree when its row's reference is set, and the reference is set anew when one would pass 2^6
+// times that: rows whose largest score grows by less than 6 (base 2) from the first tile on, which are nearly all, keep the
+// first.  A 16-bit weight is off by at most 2^-25, so 2^-34 of the largest: 10^6 keys together by 2^-14.  Float32's need no
+// such room, and scores near the reference are the more exact the nearer they are.
+template <class T> constexpr float kTopTree = std::is_same_v<T, float> ? 0.f : 9.f;
+template <class T> constexpr float kFarTree = kTopTree<T> + 6.f;
 
 template <class T> struct Octet { typedef T type __attribute__((ext_vector_type(8))); };
 
@@ -59,10 +63,12 @@ __device__ __forceinline__ uint64_t ancestors(const int32_t *parent, int m) {
 struct CodeMasks {
   uint32_t lo, hi;                       // in vector registers
   __device__ __forceinline__ CodeMasks() : lo(0x000F000Fu), hi(0x00F000F0u) { asm("" : "+v"(lo), "+v"(hi)); }
+  // C less than the codes
+  template <int C = 0>
   __device__ __forceinline__ halfx8 codes(uint32_t w) const {
     const uint32_t w8 = w >> 8;
     const uintx4 r = {(w & lo) | 0x64006400u, (w & hi) | 0x54005400u, (w8 & lo) | 0x64006400u, (w8 & hi) | 0x54005400u};
-    return __builtin_bit_cast(halfx8, r) - halfx8{1024, 1024, 64, 64, 1024, 1024, 64, 64};
+    return __builtin_bit_cast(halfx8, r) - halfx8{1024 + C, 1024 + C, 64 + C, 64 + C, 1024 + C, 1024 + C, 64 + C, 64 + C};
   }
 };
 
@@ -262,7 +268,7 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
     float mx_[NB], l[NB];                                           // reference and sum of a row's weights
     floatx4 o[NB][NT];
     constexpr bool ZS = std::is_same_v<T, float>;
-    float zs[NB][ZS ? G : 1] = {};                                  // float32: sum of p z, this lane's keys
+    float zs[NB][ZS ? G : 1] = {};                                  // float32: sum of p (z + 8 s), this lane's keys
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       mx_[n] = -INFINITY;
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
         mx = fmaxf(mx, x);
       }
       mx = col_max(mx);
-      float ref = mx - kTopTree;
+      float ref = mx - kTopTree<T>;
       if constexpr (BIG) {
         float most = 0.f;
 #pragma unroll
@@ -461,12 +467,22 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
       halfx4 kz[2] = {};
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
+        halfx8 middle = {};                                         // float32: z + 8 s in two parts
 #pragma unroll
-        for (int g = 0; g < G; ++g) kz[b][g] = half[k_zero(G, g, 16 * b + col)];
+        for (int g = 0; g < G; ++g) {
+          kz[b][g] = half[k_zero(G, g, 16 * b + col)];
+          if constexpr (ZS) {
+            const float y = fmaf(8.f, (float)half[k_scale(G, g, 16 * b + col)], (float)kz[b][g]);
+            middle[g] = (_Float16)y;
+            middle[4 + g] = (_Float16)(y - (float)middle[g]);
+          }
+        }
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           s[n][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-          if constexpr (!kHeldKeys<T>) s[n][b] = __builtin_amdgcn_mfma_f32_16x16x16f16(kz[b], qz[n], s[n][b], 0, 0, 0);
+          if constexpr (!kHeldKeys<T> && !ZS) s[n][b] = __builtin_amdgcn_mfma_f32_16x16x16f16(kz[b], qz[n], s[n][b], 0, 0, 0);
+          if constexpr (ZS)
+            s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(middle, __builtin_shufflevector(qz[n], qz[n], 0, 1, 2, 3, 4, 5, 6, 7), s[n][b], 0, 0, 0);
         }
       }
 #pragma unroll
@@ -475,7 +491,7 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
         halfx4 ks[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          kc[b] = masks.codes(tile[(b * 64 + lane) * G + g]);
+          kc[b] = masks.template codes<ZS ? 8 : 0>(tile[(b * 64 + lane) * G + g]);
           if constexpr (kHeldKeys<T>) kc[b] = kc[b] * half[k_scale(G, g, 16 * b + col)] + kz[b][g];
           else ks[b] = *(const halfx4 *)(half + k_scale(G, g, 16 * b + 4 * kq));
         }
@@ -515,13 +531,13 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx[n] = fmaxf(mx[n], s[n][e >> 2][e & 3]);
         mx[n] *= mul[n];
-        far |= mx[n] > mx_[n] + kFarTree;
+        far |= mx[n] > mx_[n] + kFarTree<T>;
       }
       if (__any(far)) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {                              // each row by its own scores alone
           const float rm = col_max(mx[n]);
-          rescale(n, rm > mx_[n] + kFarTree ? rm - kTopTree : mx_[n]);
+          rescale(n, rm > mx_[n] + kFarTree<T> ? rm - kTopTree<T> : mx_[n]);
         }
       }
 #pragma unroll
@@ -545,7 +561,7 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
           for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              zs[n][g] = fmaf(p[n][e], (float)vz[e], zs[n][g]);
+              zs[n][g] = fmaf(p[n][e], fmaf(8.f, (float)vs[e], (float)vz[e]), zs[n][g]);
               float y = p[n][e] * (float)vs[e];
 #pragma unroll
               for (int k2 = 0; k2 < 3; ++k2) {
@@ -558,7 +574,9 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
         for (int t = 2 * g; t < 2 * g + 2; ++t) {
           const uint32_t w = tile[128 * G + (t / VW * 64 + lane) * VW + t % VW];
           if constexpr (ZS) {
-            const bfx8 vc = codes_bf(w);
+            bfx8 vc;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) vc[e] = (__bf16)(float)((int)(w >> nibble_shift(e) & 15) - 8);
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
