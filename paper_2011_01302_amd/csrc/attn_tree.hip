@@ -576,7 +576,7 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
           if constexpr (ZS) {
             bfx8 vc;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) vc[e] = (__bf16)(float)((int)(w >> nibble_shift(e) & 15) - 8);
+            for (int e = 0; e < 8; ++e) vc[e] = (__bf16)(float)((int)((w ^ 0x88888888u) << (28 - nibble_shift(e))) >> 28);      // c - 8
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll

@@ -16,7 +16,7 @@ namespace ios {
 
 namespace {
 
-constexpr int kThreadsV = 1024, kThreadsD = 512, kUnrollV = 4;   // of a walk, and of a share of a row
+constexpr int kThreadsV = 1024, kThreadsD = 512, kUnrollV = 2;   // of a walk, and of a share of a row
 constexpr int kMaxShares = 64;
 
 // Where a walk stopped.
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(kThreadsD) void verify_draw_kernel(int vocab, int s
 // Workgroups that sum a row: one (and no second launch) for a small vocabulary.
 int shares_of(const ios_verify_desc &d) {
   if (d.vocab < 2 * kThreadsV * 8) return 1;
-  const int64_t want = (2048 + d.seqs - 1) / d.seqs;
+  const int64_t want = (512 + d.seqs - 1) / d.seqs;
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, kMaxShares), d.vocab / (kThreadsD * 8)));
 }
 
