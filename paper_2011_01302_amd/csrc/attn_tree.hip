@@ -19,7 +19,6 @@ constexpr int kStagesT = 3;              // tiles of a wave's ring
 constexpr int kStepTiles = kWavesT;      // tiles of a step: one a wave
 // Steps that a block of rows costs beside its keys, the fewest of a share, and the keys from which blocks are cut.
 constexpr int kItemSteps = 3, kShareSteps = 3, kOneTree = 1024;
-constexpr int64_t kRowsTree = 4096;       // rows from which a wave joins one: there are few parts of each
 
 // How the products over the cache are computed, for results in T:
 // bf16: keys and values z + s c rounded to f16 (2^-11 at most, against 2^-8 of the result), weights to f16
@@ -47,8 +46,7 @@ __device__ __forceinline__ uint64_t ancestors(const int32_t *parent, int m) {
   const int p = lane < m ? parent[lane] : -1;
   int up = p >= 0 && p < lane ? p : -1;
   uint32_t lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
+  for (int d = 1; d < m; d <<= 1) {
     const int from = max(up, 0);
     const uint32_t l = __shfl(lo, from), h = __shfl(hi, from);
     const int next = __shfl(up, from);
@@ -790,7 +788,7 @@ hipError_t run(const Call &x) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !x.groups) return e;
   const int64_t rows = x.q.tokens * d.heads, parts = 2 * (int64_t)x.groups;
-  if (rows >= kRowsTree)
+  if (parts * W <= 16 * rows)                                     // few parts of a row: a wave for each
     hipLaunchKernelGGL((attn_tree_join_kernel<T, G, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, x.s, d.heads, ratio,
                        d.seqs, x.most, W, parts, x.out, x.lse, x.cu, x.part);
   else
