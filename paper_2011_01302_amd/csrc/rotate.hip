@@ -2,7 +2,9 @@
 //
 // Every value is read and written once: bound by memory where there are many tokens, by a launch and one chain of loads
 // where there are few.  A workgroup takes a few tokens and first fills a table of their cosines and sines, which all
-// heads share, so the 64-bit work is a small part of what the values cost.
+// heads share, so the 64-bit work is a small part of what the values cost; its units are all on their way before the table
+// is, as many tokens as make four a thread.  17609 tokens of 40 heads of 128, bf16: 76 us, 4.75 TB/s (a large copy 4.9); 16
+// tokens of 10 heads of 64: 3.4.
 #include "rotary.h"
 
 namespace ios {
@@ -61,9 +63,10 @@ __global__ __launch_bounds__(256) void rotate_kernel(ios_rotary r, int head_dim,
 template <class T>
 hipError_t run(const ios_rotary &r, int head_dim, const ios_tokens &q, const ios_tokens &qo, int heads,
                const ios_tokens &k, const ios_tokens &ko, int kv_heads, const int32_t *pos, hipStream_t s) {
-  // tokens of a workgroup: up to kUnroll units a thread, but every CU has four workgroups first
+  // tokens of a workgroup: up to kUnroll units and 8 pairs of the table a thread, but every CU has four workgroups first
   const RotaryUnits u(r, head_dim);
-  const int all = heads + kv_heads, per = (int)std::max<int64_t>(1, std::min<int64_t>(256 * kUnroll / (all * u.all), q.tokens / 1024));
+  const int all = heads + kv_heads, most = std::min(256 * kUnroll / (all * u.all), 256 * 8 / u.half);
+  const int per = (int)std::max<int64_t>(1, std::min<int64_t>(most, q.tokens / 1024));
   hipLaunchKernelGGL((rotate_kernel<T>), dim3((unsigned)((q.tokens + per - 1) / per)), dim3(256),
                      per * u.half * sizeof(float2), s, r, head_dim, per, Divisor(u.all), Divisor(all), q, qo, heads, k, ko, pos);
   return hipGetLastError();

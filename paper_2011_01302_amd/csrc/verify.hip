@@ -8,6 +8,10 @@
 //
 // A workgroup walks a sequence's tree.  With a small vocabulary it also draws the next token; with a large one a second
 // launch sums that row over several workgroups, the last of which draws.
+//
+// A chain of loads and sums, each of a few hundred nanoseconds: the walk (offsets, tree, probabilities), the row, its sum
+// across the card, the share that holds the mark.  32 chains over 131072 tokens, float32: 21 us (4 for the walk, 17 for 34 MB
+// of rows, which memory alone would take 7 for); one tree over 32003 tokens 10.
 #include <type_traits>
 
 #include "decoder.h"

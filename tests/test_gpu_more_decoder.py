@@ -82,7 +82,8 @@ def rotate(typ, r, q, k, pos, qo=None, ko=None):
 
 def check_turned(typ, r, x, pos, got):
     ref, size = turned64(r, x, pos)
-    bound = TYPES[typ][2] * ref.abs() + 2.0 ** -22 * abs(r.amplitude) * size + 2.0 ** -39
+    # (numbers of f16 below 2^-14 are 2^-24 apart, so half a step is 2^-25 there and not a share of the number)
+    bound = TYPES[typ][2] * ref.abs() + 2.0 ** -22 * abs(r.amplitude) * size + (2.0 ** -25 if typ == "f16" else 2.0 ** -39)
     err = (got.double().cpu() - ref).abs()
     assert (err <= bound).all(), float((err / bound).max())
     step = turned32(r, x, pos)
@@ -112,6 +113,16 @@ def test_rotate(typ, inter, head, dim):
     k3 = k.clone()
     rotate(typ, r, k3, None, pos, k3)
     assert torch.equal(k3, ko)
+
+
+@pytest.mark.parametrize("heads,head,dim,inter,tokens", [(1, 8, 8, 1, 150001), (1, 128, 128, 0, 40000), (3, 40, 20, 0, 33333),
+                                                         (300, 8, 2, 0, 1025)])
+def test_rotate_many_tokens(heads, head, dim, inter, tokens):
+    """As many tokens a workgroup as it takes, and heads in more than one turn of its threads."""
+    r = rotary(dim, inter)
+    q, pos = randn((tokens, heads, head), torch.float16, 1), [(7 * i) % 100003 for i in range(tokens)]
+    got, _ = rotate("f16", r, q, None, pos)
+    check_turned("f16", r, q, pos, got)
 
 
 @ALL
