@@ -46,8 +46,8 @@ __device__ __forceinline__ T mean_odd(float sum, float weights) {
 
 // One workgroup of 256 threads joins row `row` of `rows`: weights of the parts first (a thread each), then four values
 // a thread, the parts spread over the threads; every sum in a fixed order.  The first loads do not wait for the number
-// of parts that hold anything (count()); the others' values are left out.  kOdd: infinities have to be expected.
-template <class T, bool kMeans, bool kOdd = kMeans, class F>
+// of parts that hold anything (count()); the others' values are left out.
+template <class T, bool kMeans, class F>
 __device__ __forceinline__ void join_parts(int64_t row, int64_t rows, int dim, int splits, const float *part, F count,
                                            T *out, float *lse) {
   static_assert(kMaxParts <= 256, "a thread per part");
@@ -91,7 +91,7 @@ __device__ __forceinline__ void join_parts(int64_t row, int64_t rows, int dim, i
     for (int u = 0; u < 8; ++u)
       if (s0 + u * W < n) {
         const float f = weight[s0 + u * W];
-        if constexpr (kOdd) {
+        if constexpr (kMeans) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] += weighed(x[u][e], f);
         } else {
@@ -107,7 +107,6 @@ __device__ __forceinline__ void join_parts(int64_t row, int64_t rows, int dim, i
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if constexpr (kMeans) r.v[e] = doubled_odd<T>(v[e]);
-      else if constexpr (kOdd) r.v[e] = mean_odd<T>(v[e], ll);
       else r.v[e] = (T)(ll == 0.f ? 0.f : v[e] / ll);
     }
     *(decltype(r) *)(out + 4 * tid) = r;

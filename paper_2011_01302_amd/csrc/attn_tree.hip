@@ -81,6 +81,7 @@ struct CodeMasks {
 struct TreeSeq {
   int64_t row;                           // its first
   int m, len, place;                     // drafts, cached tokens, slot (one that does not exist: some other's, and no tokens)
+  TreeSeq() = default;
   template <class I>
   __device__ __forceinline__ TreeSeq(const CacheView &c, const I *seqs, const I *cu, const I *lens, int i, int64_t tokens,
                                      int most) {
@@ -136,9 +137,11 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
   // the share: `left` steps from step `at` of sequence i on; without a workspace one block of rows
   int64_t share = 1, left = 1, at = blockIdx.x;
   int i = blockIdx.y;
+  TreeSeq seq;
   if (part) {
     struct Begin {
       int64_t sums[kWavesT], at;
+      TreeSeq seq;
       int i;
     };
     Begin &begin = *(Begin *)lds;
@@ -171,15 +174,22 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
       for (int64_t n; x + 1 < i1 && from >= (n = steps_of(x)); ++x) from -= n;
       begin.i = x;
       begin.at = from;
+      begin.seq = TreeSeq(c, seqs, cu, c.lens, x, q.tokens, most);
     }
     __syncthreads();
     i = __builtin_amdgcn_readfirstlane(begin.i);
     at = uniform(begin.at);
+    seq.row = uniform(begin.seq.row);
+    seq.m = __builtin_amdgcn_readfirstlane(begin.seq.m);
+    seq.len = __builtin_amdgcn_readfirstlane(begin.seq.len);
+    seq.place = __builtin_amdgcn_readfirstlane(begin.seq.place);
     __syncthreads();                                              // before the ring is filled
   }
 
+  bool known = part != nullptr;                                   // seq is sequence i
   for (int turn = 0; left > 0 && i < n_seqs;) {
-    const TreeSeq seq(c, (const_i32 *)seqs, (const_i32 *)cu, (const_i32 *)c.lens, i, q.tokens, most);
+    if (!known) seq = TreeSeq(c, (const_i32 *)seqs, (const_i32 *)cu, (const_i32 *)c.lens, i, q.tokens, most);
+    known = true;
     const int64_t a = seq.row;
     const int m = seq.m, len = seq.len, rows = m * ratio, tiles = (len + kTileKeys - 1) / kTileKeys, all = seq.block_steps();
     // which block and head of keys, from which of its steps on (the quotient is below 2^31, so its floor is right)
@@ -189,6 +199,7 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
       if (!part) return;
       ++i;
       at = 0;
+      known = false;
       continue;
     }
     const int steps = part ? (int)min((int64_t)(all - from), left) : all;

@@ -5,8 +5,6 @@
 
 namespace ios {
 
-constexpr int kMaxPairs = 64;
-
 // Cosine and sine of a position's angle, times the amplitude, rounded once from 64 bits: the angle less a multiple of
 // pi / 2 (which two numbers hold to 107 bits), then the series of both up to x^13 and x^14, off by at most 2e-14 up to
 // pi / 4.  So they round to what the definition says but for a few in 10^6, also at positions where 32 bits have lost
