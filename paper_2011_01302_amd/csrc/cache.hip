@@ -9,7 +9,8 @@
 // vector instructions, 66 per cent busy).  32 single tokens 5.6 and 3.8 us, a
 // chain of dependent loads (offsets, slot, length, page, values).  With rotation, 19136 tokens of 8 heads of 64 and 16 of
 // queries: 50 us for 130 MB (queries 23, keys and values 27, 17 unturned: vector units 60 per cent busy); 32 single tokens 6.2.
-// Accepted drafts of 256 sequences 18 us: 2048 tiles in as many places of a 1.2 GB pool.
+// Accepted drafts of 256 sequences, 2048 tiles: 12.6 us, the same chain; with a sequence's tiles beside each other 17, as every
+// other workgroup, and so half of the XCDs, had none.
 #include "rotary.h"
 
 namespace ios {
@@ -52,15 +53,15 @@ __device__ __forceinline__ TileJob find_tile(const CacheView &c, int tile_b, int
   return j;
 }
 
-// The same for the accepted drafts of sequence i, rows path[i * most ..] of the call: `per` tiles for every sequence.
+// The same for the accepted drafts of sequence i, rows path[i * most ..] of the call.
 // j.row is then the place in the list that is the tile's token 0.
 __device__ __forceinline__ TileJob find_kept(const CacheView &c, int tile_b, int n, const int32_t *seqs,
                                              const int32_t *count, int most, int head, int *seq) {
   TileJob j{nullptr, 0, 0, 0, 0};
-  const int per = most / kTileKeys + 2, i = blockIdx.x / per;
+  const int i = (int)blockIdx.x % n, x = (int)blockIdx.x / n;  // first tiles first: the others are mostly not touched
   *seq = i;
   const int slot = seqs[i], len = cache_len(c, slot), kept = (int)clip(count[i], most), first = len - kept;
-  const int p0 = max(first, 0), t0 = (p0 / kTileKeys + (int)blockIdx.x % per) * kTileKeys;
+  const int p0 = max(first, 0), t0 = (p0 / kTileKeys + x) * kTileKeys;
   if (kept == 0 || t0 >= len) return j;
   j.tile = cache_tile(c, slot, t0, head, tile_b);
   j.lo = max(p0 - t0, 0);
@@ -218,14 +219,22 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, ios_toke
       return;
     }
   }
-  // every load first: the tokens' values (a thread has up to N octets of K and of V) and the tile, if it holds some
+  // every load first: the tile, if it holds tokens, and the tokens' values (a thread has up to N octets of K and of V)
+  constexpr int I = (tile_bytes(G) / 16 + 255) / 256;
+  uintx4 *gt = (uintx4 *)j.tile, *li = (uintx4 *)img, old[I];
+#pragma unroll
+  for (int u = 0; u < I; ++u)
+    old[u] = j.lo > 0 ? gt[min(tid + 256 * u, tile_bytes(G) / 16 - 1)] : uintx4{0, 0, 0, 0};
   constexpr int N = (kTileKeys * 4 * G + 255) / 256;
   Row8<T> kr[N], vr[N];
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int o = tid + 256 * u, key = min(max(o / (4 * G), j.lo), j.hi - 1), oct = o % (4 * G);
     int64_t row = j.row + key;
-    if constexpr (M == KEPT) row = cu[(int64_t)seq * from.most + row];
+    if constexpr (M == KEPT) {
+      if (key != o / (4 * G)) continue;
+      row = cu[(int64_t)seq * from.most + row];
+    }
     if (M == KEPT && (row < 0 || row >= k.tokens)) {         // no such row: the token is 0
       kr[u] = vr[u] = Row8<T>{};
       continue;
@@ -234,8 +243,9 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, ios_toke
     vr[u] = *(const Row8<T> *)((const T *)v.data + row * v.token_stride + head * v.head_stride + oct * 8);
   }
   if constexpr (M == TURNED) turn_keys<T, G, N>(from.r, j, kr, turned, cs);
-  uintx4 *gt = (uintx4 *)j.tile, *li = (uintx4 *)img;
-  for (int i = tid; i < tile_bytes(G) / 16; i += 256) li[i] = j.lo > 0 ? gt[i] : uintx4{0, 0, 0, 0};
+#pragma unroll
+  for (int u = 0; u < I; ++u)
+    if (tid + 256 * u < tile_bytes(G) / 16) li[tid + 256 * u] = old[u];
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < N; ++u) {
