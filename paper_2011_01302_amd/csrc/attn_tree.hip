@@ -710,6 +710,11 @@ __global__ __launch_bounds__(256) void attn_tree_join_kernel(int heads, int rati
   if (ref.count <= 1) return;                                     // its workgroup has written it
   auto place = [&](int x) { return (int64_t)(x == 0 ? ref.first : (ref.first & ~1) + 2 * x) * w + (r - r0); };
   const float2 *ml = (const float2 *)(part + parts * w * D);
+  const int d4 = tid % Q, n = tid / Q, mine = n < N ? ref.count : 0;
+  floatx4 z[2];                                                   // the first values beside the references
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (n + u * N < mine) z[u] = *(const floatx4 *)(part + place(n + u * N) * D + 4 * d4);
   float top = -INFINITY, ll = 0.f;
   for (int x = tid; x < ref.count; x += TPR) top = fmaxf(top, ml[place(x)].x);
 #pragma unroll
@@ -731,16 +736,17 @@ __global__ __launch_bounds__(256) void attn_tree_join_kernel(int heads, int rati
     __syncthreads();
     ll = red[1][0] + red[1][1] + red[1][2] + red[1][3];
   }
-  const int d4 = tid % Q, n = tid / Q;
   floatx4 y = {0.f, 0.f, 0.f, 0.f};
-  if (n < N)
-#pragma unroll 4
-    for (int x = n; x < ref.count; x += N) {
-      const float f = __builtin_amdgcn_exp2f(ml[place(x)].x - mu);
-      const floatx4 z = *(const floatx4 *)(part + place(x) * D + 4 * d4);
+  auto add = [&](int x, const floatx4 &v) {
+    const float f = __builtin_amdgcn_exp2f(ml[place(x)].x - mu);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += weighed(z[e], f);
-    }
+    for (int e = 0; e < 4; ++e) y[e] += weighed(v[e], f);
+  };
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (n + u * N < mine) add(n + u * N, z[u]);
+#pragma unroll 4
+  for (int x = n + 2 * N; x < mine; x += N) add(x, *(const floatx4 *)(part + place(x) * D + 4 * d4));
   if constexpr (TPR > 64) {
     if (n < N) sum[n][d4] = y;
     __syncthreads();
