@@ -11,16 +11,18 @@ that a row sees, A = sum p (|z| + 15 s) + sum p |v| and e the largest error of a
 score, element by element:
     |o - ref| <= u |ref| + 2^-25 + (2 e + 2^-17) A + w + 2^-24 R (S + |ref|)
 e   scale (2^-22 + 2^-24 (head_dim + 8)) sum_d |q_d| (|z| + 15 s) for cached keys
-    (queries and their sums in two 16-bit parts, 32-bit sums; for bf16 the values
-    themselves may be rounded to f16, 2^-11 more), scale 2^-24 (head_dim + 10) sum |q k|
+    (queries, their sums and middles z + 8 s in two 16-bit parts or more, 32-bit sums; for
+    bf16 the values themselves may be rounded to f16, 2^-11 more), scale 2^-24 (head_dim + 10) sum |q k|
     for drafts, and 2^-17 for the exponential's argument (scores below 40) and value
-w   roundings before the second product: for bf16 p and the value to f16 (2^-10 A, and
-    2^-38 of the largest value a key for weights below f16's range); for f16 p s to two
-    16-bit parts times codes of up to 143, for float32 to three times codes of up to 15;
-    drafts' p to two parts of the type (2^-16 A)
-S   what is summed in 32 bits: A; for f16 sum p (|z| + 271 s) + sum p |v|
+w   roundings before the second product: for bf16 p and the value to f16 (2^-10 A); for f16
+    both to two f16 parts, 2^-22 each, and the product of the second parts left out, 2^-22
+    (2^-20 A); for both 2^-34 of the largest value a key for weights below f16's range; for
+    float32 p s to three 16-bit parts times codes of up to 15; drafts' p to two parts of the
+    type (2^-16 A)
+S   what is summed in 32 bits: A
 R   roundings one behind the other: 33 a tile for a quarter of the tiles at worst, 128
-    for the drafts, 8 waves, 40 for rescaling and the last steps, and 128 parts."""
+    for the drafts, 8 waves, 40 for rescaling and the last steps, and 128 for the parts (256
+    at most, over two threads at least)."""
 import math
 
 import numpy as np
@@ -351,9 +353,9 @@ def tree_reference(typ, q, kc, vc, kd, vd, see, scale):
     ac, ad = pc @ (vz.abs() + 15 * vs), pd @ v0.abs()
     ps, a = pc @ vs, ac + ad
     top = float((vz + vs * vcode).abs().max()) if m else 0.0
-    # bf16: weights are 2^9 at least where a row's largest score is, in f16, so off by half a step of 2^-11 or by 2^-25 at
-    # most: 2^-34 of the largest weight for each key, and that is at most the sum of them
-    w, summed = {"bf16": (2.0 ** -10 * ac + 2.0 ** -34 * m * top, a), "f16": (2.0 ** -16 * 143 * ps, pc @ (vz.abs() + 271 * vs) + ad),
+    # a row's largest weight is 2^9 at least where 16 bits hold it, so one is off by half a step or by 2^-25 at most: 2^-34
+    # of the largest for each key, and that is at most the sum of them
+    w, summed = {"bf16": (2.0 ** -10 * ac + 2.0 ** -34 * m * top, a), "f16": (2.0 ** -20 * ac + 2.0 ** -34 * m * top, a),
                  "f32": (2.0 ** -24 * 15 * ps, a)}[typ]
     r = 33 * -(-m // 128) + 128 + 8 + 40 + 128
     fine = torch.where(torch.isfinite(out), out, 0.0).abs()
@@ -926,3 +928,26 @@ def test_step_in_a_graph():
                 kept = outs[0]["path"][row, :int(outs[0]["count"][row])].long()
                 assert equal(a[0][m - len(kept):], held(outs[0]["k"][kept])) and equal(a[1][m - len(kept):], held(x["v"][kept]))
     assert I.ios_cache_status(caches[0].c, stream()) == 0
+
+
+def test_example_drafts():
+    """The example's path, end to end: what stood is what the cache grew by, and the same comes out again."""
+    import importlib.util
+    import os
+    import sys
+    folder = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples")
+    spec = importlib.util.spec_from_file_location("draft_answers", os.path.join(folder, "draft_answers.py"))
+    ex = importlib.util.module_from_spec(spec)
+    before = list(sys.path)
+    try:
+        spec.loader.exec_module(ex)
+    finally:
+        sys.path[:] = before
+    ids, stood, dec = ex.answers(3, 6)
+    assert len(stood) == 6 and all(1 <= x <= 4 for row in stood for x in row)
+    counts = [sum(row[i] for row in stood) for i in range(3)]
+    assert [len(r) for r in ids] == counts and len({r[0] for r in ids}) == 3
+    assert all(0 <= t < ex.VOCAB for r in ids for t in r)
+    assert dec.lens.tolist() == [1225] + [1225 + m for m in counts]
+    again = ex.answers(3, 6)
+    assert again[0] == ids and again[1] == stood
