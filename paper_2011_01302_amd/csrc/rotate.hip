@@ -66,7 +66,8 @@ hipError_t run(const ios_rotary &r, int head_dim, const ios_tokens &q, const ios
   // tokens of a workgroup: up to kUnroll units and 8 pairs of the table a thread, but every CU has four workgroups first
   const RotaryUnits u(r, head_dim);
   const int all = heads + kv_heads, most = std::min(256 * kUnroll / (all * u.all), 256 * 8 / u.half);
-  const int per = (int)std::max<int64_t>(1, std::min<int64_t>(most, q.tokens / 1024));
+  // (a grid has less than 2^32 threads)
+  const int per = (int)std::max<int64_t>((q.tokens >> 23) + 1, std::min<int64_t>(most, q.tokens / 1024));
   hipLaunchKernelGGL((rotate_kernel<T>), dim3((unsigned)((q.tokens + per - 1) / per)), dim3(256),
                      per * u.half * sizeof(float2), s, r, head_dim, per, Divisor(u.all), Divisor(all), q, qo, heads, k, ko, pos);
   return hipGetLastError();
