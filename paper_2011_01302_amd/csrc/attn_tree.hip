@@ -44,6 +44,14 @@ template <class T> constexpr int kQueryParts = std::is_same_v<T, float> ? 3 : 1;
 template <class T> constexpr float kTopTree = std::is_same_v<T, float> ? 0.f : 9.f;
 template <class T> constexpr float kFarTree = kTopTree<T> + 6.f;
 
+// Rows in which a draft's value times such a weight would come near float32's largest hold their sums 2^-kApart times as
+// large.  Float32 simply takes a reference so much higher; in bf16 the cached tokens' weights go to f16, which has no room
+// for that (weights of 2^-24 and less are its last subnormal number or 0, and the row's ordinary values lose most of what the
+// wave that has the drafts adds, an eighth), so there the weights stay as they are and the products of such rows are taken
+// by themselves.  The test for them costs 1 per cent (one sequence of 131072 tokens 75.7 and 76.3 us).
+template <class T> constexpr float kApart = kTopTree<T> + 24.f;
+template <class T> constexpr bool kApartSums = std::is_same_v<T, __bf16>;
+
 template <class T> struct Octet { typedef T type __attribute__((ext_vector_type(8))); };
 
 // Which drafts of its sequence draft `lane` sees: itself and its ancestors.  A parent that is not an earlier draft is
@@ -294,6 +302,8 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
     }
 
     // the drafts' own keys, a tile of them and 16 rows for each wave, from the last wave on; every load first
+    constexpr float kDown = 1.0 / (1ull << (int)kApart<T>);
+    uint64_t apart = 0;                                             // lanes of rows `my` whose sums are kDown times as large
     const int my = (kWavesT - 1 - wave) % NB, k0 = (kWavesT - 1 - wave) / NB * kTileKeys;
     if (from == 0 && k0 < m && r0 + 16 * my < rows) {
       const T *kd = (const T *)k.data + a * k.token_stride + kvh * k.head_stride;
@@ -364,8 +374,7 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, top[e]);
         if (__any(most > 0x1p90f)) {
-          // rows whose products would come near float32's largest take weights up to 2^-24; a large value of no weight
-          // leaves the others' weights where 16 bits hold them
+          // (a large value of no weight leaves its rows as they are)
           float far = -INFINITY;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -374,7 +383,9 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
             for (int y = 1; y < 16; y <<= 1) x = fmaxf(x, __shfl_xor(x, y));
             far = fmaxf(far, __builtin_log2f(x) + (s[e >> 2][e & 3] - mx));
           }
-          if (col_max(far) > 100.f) ref = mx + 24.f;
+          far = col_max(far);
+          if constexpr (kApartSums<T>) apart = __ballot(far > 100.f);
+          else if (far > 100.f) ref += kApart<T>;
         }
       }
       float p[8], sum = 0.f;
@@ -382,6 +393,10 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
       for (int e = 0; e < 8; ++e) {
         p[e] = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] - (ref == -INFINITY ? 0.f : ref));
         sum += p[e];
+      }
+      if (kApartSums<T> && apart) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] *= apart >> lane & 1 ? kDown : 1.f;
       }
       floatx4 od[NT];
 #pragma unroll
@@ -549,11 +564,37 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
         mx[n] *= mul[n];
         far |= mx[n] > mx_[n] + kFarTree<T>;
       }
-      if (__any(far)) {
+      if (__any(far) || apart) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {                              // each row by its own scores alone
           const float rm = col_max(mx[n]);
           rescale(n, rm > mx_[n] + kFarTree<T> ? rm - kTopTree<T> : mx_[n]);
+        }
+        if (kApartSums<T> && apart) {                               // products by themselves, no weight in those below
+          halfx8 pa = {};
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+            if (n == my) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float y = s[n][e >> 2][e & 3];
+                const float x = apart >> lane & 1 ? __builtin_amdgcn_exp2f(fmaf(y, mul[n], -mx_[n])) : 0.f;
+                l[n] += x;
+                pa[e] = (_Float16)x;
+                s[n][e >> 2][e & 3] = apart >> lane & 1 ? -INFINITY : y;
+              }
+            }
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            asm volatile("" ::: "memory");                          // one after the other: few registers
+            const halfx8 vs = *(const halfx8 *)(tile + v_param(G, t / 2, kq)), vz = *(const halfx8 *)(tile + v_param(G, t / 2, kq) + 4);
+            const halfx8 vv = masks.codes(tile[128 * G + (t / VW * 64 + lane) * VW + t % VW]) * vs + vz;
+            const floatx4 y = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pa, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+              if (n == my) o[n][t] += y * kDown;
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
       }
 #pragma unroll
@@ -619,6 +660,14 @@ __global__ __launch_bounds__(kThreadsT) void attn_tree_kernel(CacheView c, int h
           }
         }
       }
+    }
+    if (kApartSums<T> && apart) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+        if (n == my && (apart >> lane & 1)) {
+          l[n] *= kDown;
+          mx_[n] += kApart<T>;
+        }
     }
 #pragma unroll
     for (int n = 0; n < NB; ++n) {                                  // o[n][t][r] is value 16 t + 4 kq + r of row col

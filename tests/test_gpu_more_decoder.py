@@ -547,6 +547,39 @@ def test_tree_large_value_of_no_weight(typ, size, low):
     assert (out[1:4].abs() < 100).all() and (out[4:, :, 9] < -2.0 ** 13).all()
 
 
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("large", [2.0 ** 104, 3.0e38, math.inf])
+@pytest.mark.parametrize("lead", [4.0, -20.0])
+@pytest.mark.parametrize("dim,kv,ratio,drafts,bound", [(64, 1, 4, 6, 2500), (32, 2, 1, 40, 2500), (96, 1, 16, 5, 2500),
+                                                       (64, 8, 8, 8, 0)])
+def test_tree_one_large_value_among_ordinary_ones(typ, large, lead, dim, kv, ratio, drafts, bound):
+    """A draft with one very large value: the other values of the rows that see it, which are mostly the cache's, stay within
+    the bounds of ordinary ones; rows that do not see it stay as they are to the bit.  Drafts score 4 (base 2) above the
+    cached tokens, or 20 below; the cached values are 2 in the mean, and each of a workgroup's waves has an eighth of that."""
+    print("\n[gpu-case] tree one large value", typ, large, lead, dim, kv, ratio, drafts, flush=True)
+    dt, lens, who = TYPES[typ][0], [2500, 300], drafts - 2
+    c = Cache(kv, dim, 64, 50, 3, 40)
+    c.place(lens, 31)
+    kc, vc = randn((2800, kv, dim), torch.float32, 31), randn((2800, kv, dim), torch.float32, 32) + 2.0
+    c.append(kc, vc, [0, 1], lens, "f32")
+    hk, hv = ([[t[:2500] for t in quantised(x)], [t[2500:] for t in quantised(x)]] for x in (kc, vc))
+    parents = [forest(drafts, np.random.default_rng(drafts + i), "tree") for i in range(2)]
+    parents[0][drafts - 1] = who
+    flat, n, cu = parents[0] + parents[1], 2 * drafts, [0, drafts, 2 * drafts]
+    q, k, v = randn((n, kv * ratio, dim), dt, 5, 0.25), randn((n, kv, dim), dt, 6), randn((n, kv, dim), dt, 7)
+    q[:, :, 0], k[:, :, 0] = 4.0, lead * math.log(2.0) / (4.0 * 2.0 ** -5)
+    big = v.clone()
+    big[who, :, 9], big[drafts, 0, 3] = large, -large
+    see = torch.zeros(n, dtype=torch.bool)
+    see[:drafts], see[drafts:] = visible(parents[0])[:, who], visible(parents[1])[:, 0]
+    assert see.any() and not see.all()
+    for work in (True, False):
+        clean, _, _ = tree(typ, c, q, k, v, [0, 1], cu, flat, drafts, max_keys=bound, work=work, scale=2.0 ** -5)
+        got = check_tree(typ, c, q, k, big, [0, 1], [drafts] * 2, parents, hk, hv, max_keys=bound, work=work, scale=2.0 ** -5)
+        assert torch.equal(got[~see.to(DEV)], clean[~see.to(DEV)])
+        assert torch.isfinite(got[:, :, 10:]).all()
+
+
 @pytest.mark.parametrize("typ", ["bf16", "f16"])
 @pytest.mark.parametrize("bound", [5000, 0])
 def test_tree_ragged_batch(typ, bound):
