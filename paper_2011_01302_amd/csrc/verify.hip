@@ -376,7 +376,7 @@ hipError_t launch_verify(const ios_verify_desc &d, const ios_rows &p, const ios_
                        tokens, parent, cu, accept, sample, path, count, next, stop);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int share = ((d.vocab + shares - 1) / shares + 7) / 8 * 8;
+    const int share = (int)((((int64_t)d.vocab + shares - 1) / shares + 7) / 8 * 8);
     hipLaunchKernelGGL((verify_draw_kernel<T, GIVEN>), dim3(shares, d.seqs), dim3(kThreadsD), 0, s, d.vocab, share, p, qq,
                        sample, next, stop);
     return hipGetLastError();

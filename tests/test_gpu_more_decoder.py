@@ -825,6 +825,21 @@ def test_verify_large_vocabulary_and_strides(typ, given):
                  uniform(15, 7), uniform(2, 8))
 
 
+@pytest.mark.parametrize("given", [False, True])
+def test_verify_largest_vocabulary(given):
+    """2^31 - 1 tokens, all but four without a probability: the draw is from what a rejected draft leaves, not from p."""
+    vocab = 2 ** 31 - 1
+    p = torch.zeros(1, vocab, dtype=torch.bfloat16, device=DEV)
+    p[0, 5], p[0, 77], p[0, 2 ** 30], p[0, vocab - 1] = 0.5, 0.125, 0.25, 0.125
+    q = torch.zeros(1, vocab, dtype=torch.bfloat16, device=DEV) if given else None
+    if given:
+        q[0, 5] = 1.0
+    for sample, token in ((0.1, 77), (0.25, 2 ** 30), (0.7, 2 ** 30), (0.9, vocab - 1)):      # of 1/8, 1/4 and 1/8
+        path, count, following = verify("bf16", p.expand(2, vocab), q.expand(2, vocab) if given else None, [0, 5], [-1, 0],
+                                        [0, 2], torch.full((2,), 0.75, device=DEV), torch.full((1,), sample, device=DEV), 2)
+        assert path.tolist() == [[0, -1]] and count.tolist() == [1] and following.tolist() == [token]
+
+
 @ALL
 @pytest.mark.parametrize("given", [True, False])
 def test_verify_edges(typ, given):
