@@ -579,7 +579,8 @@ int ios_attn_cache(const ios_cache *c, int32_t layer, const ios_attn_desc *d, co
  * work_bytes) may be NULL; it needs no initial values, and
  * ios_attn_tree_work_bytes says how much spreads long caches over workgroups
  * (by all sequences' lengths, so the last bits of a row depend on the others).
- * Errors: as ios_attn_cache. */
+ * Errors: as ios_attn_cache; of both calls, IOS_E_UNSUPPORTED where max_drafts
+ * times heads is above 65535 or q->tokens times heads above 2^25 - 1. */
 int ios_attn_tree_work_bytes(const ios_attn_desc *d, int64_t q_tokens, int32_t max_drafts, int64_t *bytes);
 int ios_attn_tree(const ios_cache *c, int32_t layer, const ios_attn_desc *d, const ios_tokens *q, const ios_tokens *k,
                   const ios_tokens *v, const ios_tokens *out, float *lse, const int32_t *seqs, const int32_t *cu,

@@ -861,7 +861,7 @@ hipError_t run(const Call &x) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !x.groups) return e;
   const int64_t rows = x.q.tokens * d.heads, parts = 2 * (int64_t)x.groups;
-  if (parts * W <= 16 * rows)                                     // few parts of a row: a wave for each
+  if (parts * W <= 16 * rows)                                     // few parts of a row: a wave for each, always from 2048 rows on
     hipLaunchKernelGGL((attn_tree_join_kernel<T, G, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, x.s, d.heads, ratio,
                        d.seqs, x.most, W, parts, x.out, x.lse, x.cu, x.part);
   else

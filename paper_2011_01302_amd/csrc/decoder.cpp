@@ -170,6 +170,11 @@ void check_drafts(int32_t most) {
   need(most >= 1 && most <= kMaxDrafts, IOS_E_ARG, "drafts of a sequence must be 1 to 64");
 }
 
+// Rows of all heads, as many as fit a grid of a wave each (fewer than 2^32 threads), and of one sequence.
+void check_tree(const ios_attn_desc &d, int64_t q_tokens, int32_t most) {
+  need(q_tokens * d.heads <= INT32_MAX / 64 && (int64_t)most * d.heads <= 65535, IOS_E_UNSUPPORTED, "too many rows and heads");
+}
+
 void check_rows(const ios_rows *t, const ios_verify_desc *d, const char *what) {
   const std::string w(what);
   if (!t) fail(IOS_E_ARG, w + ": null matrix");
@@ -379,6 +384,7 @@ extern "C" int ios_attn_tree_work_bytes(const ios_attn_desc *d, int64_t q_tokens
     check_drafts(max_drafts);
     need(bytes != nullptr, IOS_E_ARG, "null bytes");
     need(q_tokens >= 0 && q_tokens <= kMaxTokens, IOS_E_ARG, "q_tokens out of range");
+    check_tree(*d, q_tokens, max_drafts);
     *bytes = tree_bytes(*d, q_tokens, max_drafts);
   });
 }
@@ -401,8 +407,7 @@ extern "C" int ios_attn_tree(const ios_cache *c, int32_t layer, const ios_attn_d
     need(seqs && cu && parent, IOS_E_ARG, "null list");
     const CacheView cv = view(*c, layer);
     if (q->tokens == 0) return;
-    need(q->tokens * d->heads <= INT32_MAX / 256 && (int64_t)max_drafts * d->heads <= 65535, IOS_E_UNSUPPORTED,
-         "too many rows and heads");
+    check_tree(*d, q->tokens, max_drafts);
     need(!work || (aligned16(work) && work_bytes >= tree_bytes(*d, q->tokens, max_drafts)), IOS_E_ARG,
          "workspace below ios_attn_tree_work_bytes or misaligned");
     launched(launch_attn_tree(cv, *d, *q, *k, *v, *out, lse, seqs, cu, parent, max_drafts, work, (hipStream_t)hip_stream),

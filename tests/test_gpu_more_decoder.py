@@ -606,6 +606,28 @@ def test_tree_more_sequences_than_threads():
     check_tree("f16", c, q, k, v, [(7 * i) % 43 - 1 for i in range(1300)], drafts, parents, hk, hv)
 
 
+@pytest.mark.parametrize("work", [True, False])
+def test_tree_more_rows_than_a_workgroup_each(work):
+    """8192 sequences under 32 drafts of 32 heads, 2^23 rows in all; every four sequences are the same."""
+    n, drafts, heads, dim, lens = 8192, 32, 32, 32, [1100, 40, 0, 300]
+    print("\n[gpu-case] tree of 2^23 rows", work, flush=True)
+    c, hk, hv = cached(1, dim, 32, lens, 41)
+    parents = [forest(drafts, np.random.default_rng(i), kind) for i, kind in enumerate(["tree", "chain", "roots", "tree"])]
+    q, k, v = (randn((4 * drafts, h, dim), torch.float16, s) for h, s in ((heads, 1), (1, 2), (1, 3)))
+    out, lse, scale = tree("f16", c, *(t.repeat(n // 4, 1, 1) for t in (q, k, v)), [0, 1, 2, 3] * (n // 4),
+                           [drafts * i for i in range(n + 1)], [p for t in parents for p in t] * (n // 4), drafts, max_keys=1100,
+                           work=work)
+    out, lse = out.view(n // 4, 4, drafts, heads, dim), lse.view(heads, n // 4, 4, drafts)
+    for i in range(4):
+        rows, see = slice(drafts * i, drafts * i + drafts), visible(parents[i])
+        for h in range(heads):
+            ref, l64, bound, far = (t.to(DEV) for t in tree_reference("f16", q[rows, h], [x[:, 0] for x in hk[i]],
+                                                                      [x[:, 0] for x in hv[i]], k[rows, 0], v[rows, 0], see, scale))
+            err = (out[:, i, :, h].double() - ref).abs()
+            assert (err <= bound).all(), (i, h, float((err / bound).max()))
+            assert ((lse[h, :, i].double() - l64).abs() <= far).all(), (i, h)
+
+
 @ALL
 @pytest.mark.parametrize("lead", [11.5, 18.0])
 def test_tree_long_tail(typ, lead):

@@ -188,6 +188,19 @@ def test_tree():
     assert I.ios_attn_tree_work_bytes(desc(seqs=1, max_keys=64), 10, 8) == 0
 
 
+def test_tree_refuses_the_same_sizes_in_both_calls():
+    """Rows and heads that no launch takes are refused before a workspace is allocated for them."""
+    def call(d, n, most):
+        I.ios_attn_tree(cache(), 0, d, toks(n=n), toks(2, n=n), toks(2, n=n), toks(n=n), 0, P, P, P, most, 0, 0)
+    most_rows = 2 ** 25 - 1                    # of all heads, as documented
+    for d, n, most in ((desc(heads=8192), 10, 64), (desc(heads=1024), 10, 64), (desc(heads=8), most_rows // 8 + 1, 8),
+                       (desc(heads=16384), 2048, 3)):
+        refused("IOS_E_UNSUPPORTED", I.ios_attn_tree_work_bytes, d, n, most)
+        refused("IOS_E_UNSUPPORTED", lambda d=d, n=n, most=most: call(d, n, most))
+    for d, n, most in ((desc(heads=1022), 10, 64), (desc(heads=8), most_rows // 8, 8), (desc(heads=32), 8192 * 32, 32)):
+        assert I.ios_attn_tree_work_bytes(d, n, most) > 0
+
+
 # ---------------------------------------------------------------- the check of drafts
 
 def test_verify():
