@@ -448,8 +448,9 @@ int ios_attn_prompt(const ios_attn_desc *d, const ios_tokens *q, const ios_token
  * (of 10^6 of them a few may be the neighbouring float32 number), then in
  * float32, each step rounded to nearest even, and to the tensor's type:
  *     a' = f32(a c) - f32(b s),  b' = f32(a s) + f32(b c).
- * The other values of a head stay as they are.  freq negated turns back, which
- * is also the gradient (where the amplitude is 1; times its square if not). */
+ * The other values of a head stay as they are.  With freq negated a result's
+ * gradient becomes the input's, and with the amplitude's inverse as well a
+ * result its input. */
 typedef struct {
   int32_t dim;               /* even, from 2 to the head's size                        */
   int32_t interleaved;       /* 1 = pairs of neighbours, 0 = of halves                 */

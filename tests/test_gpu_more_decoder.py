@@ -162,6 +162,41 @@ def test_rotate_gradient_is_the_rotation_back(typ):
 
 
 @ALL
+@pytest.mark.parametrize("inter,dim,amplitude", [(0, 64, 1.0), (1, 40, 1.25), (0, 20, 0.75)])
+def test_rotate_gradient_by_type_and_differences(typ, inter, dim, amplitude):
+    """Of L(x) = <turn(x), y> the gradient is y turned with the frequencies negated: against differences of L along
+    directions z.  x and z are eighths, so x + z and x - z are exact in every type, and L(x + z) - L(x - z) = 2 <z, gradient>
+    but for each call's own roundings (as check_turned counts them), weighed by y and by 2 |z|."""
+    n, dt = 9, TYPES[typ][0]
+    pos = [0, 1, 3, 70, 1000, 12345, 100003, -5, 7]
+    rng = np.random.default_rng(dim)
+    eighths = lambda: torch.from_numpy(rng.integers(-16, 17, (n, 2, 64)) / 8.0).to(dt).to(DEV)  # noqa: E731
+    x, y, r = eighths(), randn((n, 2, 64), dt, 2), rotary(dim, inter, amplitude)
+
+    def bound(t):
+        ref, size = turned64(r, t, pos)
+        return TYPES[typ][2] * ref.abs() + 2.0 ** -22 * amplitude * size + (2.0 ** -25 if typ == "f16" else 2.0 ** -39)
+    turned = {}
+    zs = [eighths() for _ in range(4)]
+    for i, z in enumerate(zs):
+        turned[i] = [(rotate(typ, r, t, None, pos)[0].double().cpu(), bound(t)) for t in (x + z, x - z)]
+    for i in range(dim // 2):
+        r.freq[i] = -r.freq[i]
+    grad, off = rotate(typ, r, y, None, pos)[0].double().cpu(), bound(y)
+    y = y.double().cpu()
+    for i, z in enumerate(zs):
+        (a, ea), (b, eb) = turned[i]
+        z = z.double().cpu()
+        err = float(((a - b) * y).sum() - 2 * (z * grad).sum())
+        assert abs(err) <= float(((ea + eb) * y.abs()).sum() + 2 * (z.abs() * off).sum()), (i, err)
+        # and one pair alone, where errors cannot cancel: direction z in it, the loss its two values times y
+        at = i % (dim // 2)
+        pair = [2 * at, 2 * at + 1] if inter else [at, at + dim // 2]
+        err = ((a - b) * y)[..., pair].sum(-1) - 2 * (z * grad)[..., pair].sum(-1)
+        assert (err.abs() <= ((ea + eb) * y.abs())[..., pair].sum(-1) + 2 * (z.abs() * off)[..., pair].sum(-1)).all(), i
+
+
+@ALL
 def test_rotate_strides(typ):
     """Slices of a joint projection, heads before tokens, one row for all tokens; outputs in a joint tensor."""
     dt, n = TYPES[typ][0], 33
