@@ -642,6 +642,36 @@ def test_tree_more_sequences_than_threads():
 
 
 @pytest.mark.parametrize("work", [True, False])
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, 1e-35, -1e-35])
+def test_tree_large_scores_of_a_small_scale(typ, scale, work):
+    """Scores of 10^35 and more weigh as the definition says, also times 0."""
+    dt = TYPES[typ][0]
+    c, hk, hv = cached(1, 32, 32, [1100, 40], 43)
+    parents = [forest(9, np.random.default_rng(i), "tree") for i in range(2)]
+    q, k, v = (randn((18, h, 32), torch.float32, s, size).to(dt) for h, s, size in ((3, 1, 1e17), (1, 2, 1e17), (1, 3, 1.0)))
+    check_tree(typ, c, q, k, v, [0, 1], [9, 9], parents, hk, hv, max_keys=1100, work=work, scale=scale)
+
+
+@pytest.mark.parametrize("work", [True, False])
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("where", ["cache", "drafts"])
+def test_tree_scores_beyond_float32_are_not_zeros(typ, where, work):
+    """Where scores times log2(e) leave float32's range there is no result; it reads as NaN, not as a row of zeros."""
+    dt = TYPES[typ][0]
+    c = Cache(1, 32, 32, 40, 1, 36)
+    c.place([1100])
+    k = torch.full((1100, 1, 32), 2.0, device=DEV)
+    k[1::2] = 1.0
+    c.append(k, randn((1100, 1, 32), torch.float32, 2), [0], [1100], "f32")
+    q = torch.full((6, 2, 32), 2.0 ** 122 if where == "cache" else 2.5e18, dtype=dt, device=DEV)      # scores of 3e38
+    kd = torch.full((6, 1, 32), 0.0 if where == "cache" else 2.5e18, dtype=dt, device=DEV)
+    out, lse, _ = tree(typ, c, q, kd, randn((6, 1, 32), dt, 3), [0], [0, 6], [-1, 0, 1, 1, 3, -1], 6, max_keys=1100, work=work,
+                       scale=1.5)
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+@pytest.mark.parametrize("work", [True, False])
 def test_tree_more_rows_than_a_workgroup_each(work):
     """8192 sequences under 32 drafts of 32 heads, 2^23 rows in all; every four sequences are the same."""
     n, drafts, heads, dim, lens = 8192, 32, 32, 32, [1100, 40, 0, 300]
@@ -946,6 +976,27 @@ def test_verify_keeps_the_models_distribution():
         if given:
             assert ((got - p1.double()).abs() <= 5 * torch.sqrt(p1 * (1 - p1) / n).double() + 1e-6).all(), got
         assert 0.2 < float((count == 2).float().mean()) < 0.98
+
+
+@pytest.mark.parametrize("tokens", ["fixed", "any"])
+def test_verify_certain_drafts_keep_the_models_distribution(tokens):
+    """The same without draft probabilities: whatever the drafted tokens are, the one that comes out is distributed as p."""
+    vocab, n, m = 6, 65000, 4
+    p1 = torch.tensor([0.02, 0.4, 0.05, 0.3, 0.13, 0.1])
+    p = p1.to(DEV).expand(n * m, vocab)
+    if tokens == "fixed":
+        drafts = torch.tensor([0, 1, 4, 3]).repeat(n)
+    else:                                              # a token twice among them
+        drafts = torch.randint(0, vocab, (n * m,), generator=torch.Generator().manual_seed(1))
+    path, count, following = verify("f32", p, None, drafts.tolist(), [-1, 0, 0, 0] * n, [m * i for i in range(n + 1)],
+                                    uniform(n * m, 2), uniform(n, 3), m)
+    assert int(count.min()) == 1 and int(count.max()) == 2
+    second = torch.where(count == 2, drafts.to(DEV)[path[:, 1].clamp(min=0).long()].int(), following).cpu()
+    got = torch.bincount(second.long(), minlength=vocab).double() / n
+    assert ((got - p1.double()).abs() <= 5 * torch.sqrt(p1 * (1 - p1) / n).double() + 1e-6).all(), got
+    stood = float((count == 2).float().mean())
+    if tokens == "fixed":                              # 0.4 + 0.13 + 0.3
+        assert abs(stood - 0.83) <= 5 * math.sqrt(0.83 * 0.17 / n)
 
 
 # ---------------------------------------------------------------- together
