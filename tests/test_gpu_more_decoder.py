@@ -784,6 +784,70 @@ def test_tree_in_a_graph_with_other_lengths():
         check_tree("f16", c, q, k, v, order, drafts, parents, hk, hv, max_keys=4000)
 
 
+# ---------------------------------------------------------------- offsets that pass 32 bits
+
+def test_pool_beyond_32_bits():
+    """Drafts over, rotated appends into and drafts kept in pages that lie more than 4 GiB apart."""
+    c = Cache(8, 128, 256, 16000, 2, 16)
+    assert c.pool.numel() > 1 << 32
+    lens = [3000, 500]
+    c.place(lens, 3)
+    assert int(c.table[c.table >= 0].max()) * c.pool.shape[2] > 1 << 32
+    x, v = (randn((3500, 8, 128), torch.bfloat16, s) for s in (1, 2))
+    r, seqs, cu = rotary(128), i32([0, 1]), i32([0, 3000, 3500])
+    q = randn((3500, 8, 128), torch.bfloat16, 4)
+    qo = torch.empty_like(q)
+    I.ios_cache_append_rotary(c.c, 0, I.IOS_BF16, r, toks(q), toks(qo), 8, toks(x), toks(v), 2, seqs.data_ptr(), cu.data_ptr(),
+                              stream())
+    torch.cuda.synchronize()
+    want_q, k = rotate("bf16", r, q, x, list(range(3000)) + list(range(500)))
+    gk, gv = c.read([0, 1], lens)
+    assert torch.equal(qo, want_q) and equal(gk, held(k)) and equal(gv, held(v))
+    hk, hv = ([[t[:3000] for t in quantised(y.float())], [t[3000:] for t in quantised(y.float())]] for y in (k, v))
+    parents = [forest(6, np.random.default_rng(i), "tree") for i in range(2)]
+    qd, kd, vd = (randn((12, 8, 128), torch.bfloat16, s) for s in (5, 6, 7))
+    for work in (True, False):
+        check_tree("bf16", c, qd, kd, vd, [0, 1], [6, 6], parents, hk, hv, max_keys=3000, work=work)
+    path, count = i32([[0, 2, 5], [6, 7, -1]]), i32([3, 2])
+    I.ios_cache_keep(c.c, 0, I.IOS_BF16, toks(kd), toks(vd), 2, seqs.data_ptr(), path.data_ptr(), 3, count.data_ptr(), stream())
+    torch.cuda.synchronize()
+    gk, gv = c.read([0, 1], [3, 2])
+    assert equal(gk, held(kd[[0, 2, 5, 6, 7]])) and equal(gv, held(vd[[0, 2, 5, 6, 7]]))
+
+
+def test_rows_beyond_32_bits():
+    """Rows 8 MiB apart, heads in turn 4 GiB apart: the same bits as from rows beside each other."""
+    n, heads, kv, dim, dt = 600, 4, 2, 64, torch.bfloat16
+    q, k, v = randn((n, heads, dim), dt, 1), randn((n, kv, dim), dt, 2), randn((n, kv, dim), dt, 3)
+    room = torch.empty(n * (1 << 22), dtype=dt, device=DEV)
+
+    def far(t, at):
+        y = room.as_strided(t.shape, (1 << 22, t.shape[2], 1), at)
+        y.copy_(t)
+        return y
+    fq, fk, fv, fo = far(q, 0), far(k, 4096), far(v, 8192), far(q, 12288)
+    r, pos = rotary(dim), [3 * i for i in range(n)]
+    want_q, want_k = rotate("bf16", r, q, k, pos)
+    rotate("bf16", r, fq, fk, pos, fq, fk)
+    assert torch.equal(fq, want_q) and torch.equal(fk, want_k)
+    c, hk, hv = cached(kv, dim, 32, [1200, 70], 5)
+    drafts, d = [15] * 40, desc("bf16", heads, kv, dim, 40, 0, 1200)
+    seqs, cu, parent = i32([0, 1] * 20), i32(offsets(drafts)), i32([j - 1 for j in range(15)] * 40)
+    size = I.ios_attn_tree_work_bytes(d, n, 15)
+    work, out = torch.zeros(size, dtype=torch.uint8, device=DEV), torch.empty_like(q)
+    for a, b, e, o in ((want_q, want_k, v, out), (fq, fk, fv, fo)):
+        I.ios_attn_tree(c.c, 0, d, toks(a), toks(b), toks(e), toks(o), 0, seqs.data_ptr(), cu.data_ptr(), parent.data_ptr(), 15,
+                        work.data_ptr(), size, stream())
+    torch.cuda.synchronize()
+    assert torch.equal(out, fo)
+    del fq, fk, fv, fo, room
+    # one head 4 GiB behind the other
+    room = torch.empty(2, 1 << 31, dtype=dt, device=DEV)
+    k2 = room.as_strided((n, kv, dim), (dim, 1 << 31, 1))
+    k2.copy_(k)
+    assert torch.equal(rotate("bf16", r, k2, None, pos, k2)[0], want_k)
+
+
 # ---------------------------------------------------------------- the check of drafts
 
 def walk(p, q, tokens, parent, accept, sample):
