@@ -576,7 +576,9 @@ int ios_attn_cache(const ios_cache *c, int32_t layer, const ios_attn_desc *d, co
  * sequence, its ancestors and itself; a draft that it does not see never
  * changes it, not even by a NaN.  Nothing is written to the cache.  lse as
  * ios_attn_prompt, [heads][q->tokens]; causal is not read.  Drafts' keys and
- * values are read as they are, cached ones as they are held.  `work` (of
+ * values are read as they are, cached ones as they are held.  A weight counts to
+ * within 2^-34 of its row's largest in f16, and for cached tokens in bf16, and
+ * otherwise down to 2^-90 of it (infinite values always do).  `work` (of
  * work_bytes) may be NULL; it needs no initial values, and
  * ios_attn_tree_work_bytes says how much spreads long caches over workgroups
  * (by all sequences' lengths, so the last bits of a row depend on the others).

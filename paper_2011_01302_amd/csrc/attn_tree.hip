@@ -10,11 +10,16 @@
 // lies in several shares leaves its parts in the workspace, at most two a workgroup, for a second launch.  (Parts by the
 // longest sequence's length left workgroups idle for 39 per cent of the time on 32 sequences of 8192 to 32031 tokens.)
 //
-// Those under 16 drafts of 32 heads (64 rows a head of keys, bf16): 290 us, 823 MB of cache and 169 GFLOP, of which the matrix
-// cores take 25 and the vector units 50 per cent (codes to numbers and the softmax); two waves a SIMD, as many as the sums'
-// registers leave room for, do not cover the rest.  Under 4 drafts (16 rows) 167 us: memory.  One sequence of 131072 tokens
-// under 32 drafts of 16 heads 76 us.  A small call is latency: 28x28 tokens under 7 drafts 19 us, four tiles a wave one after
-// the other, before and after them the queries, the drafts and the join of the waves with code that no cache holds yet.
+// Those under 16 drafts of 32 heads (64 rows a head of keys, bf16): 290 us, 823 MB of cache and 169 GFLOP.  Matrix cores are
+// busy for 25 and vector units (codes to numbers and the softmax) for 50 per cent, waves wait for 38: a tile's scores, weights
+// and values follow each other, and two waves a SIMD, as many as the sums' registers leave room for, do not cover that.  f16
+// takes 530 (values formed in 32 bits and split one by one, three products for one), float32 880.  Under 4 drafts (16 rows)
+// 166 us: memory.  One sequence of 131072 tokens under 32 drafts of 16 heads 76 us, four blocks of rows that each turn the same
+// codes into numbers.  A small call is latency: 28x28 tokens under 7 drafts 19 us, four tiles a wave one after the other, before
+// and after them the queries, the drafts and the join of the waves with code that no cache holds yet.
+//
+// Every workgroup reads all sequences' offsets and lengths to find its share, and steps over those without rows one by one: 32
+// drafts behind 32 sequences of 40 tokens 15 us, behind 32 of 4096 94 and of 65535 1435 (39 and 330 without a workspace).
 #include "attn_codes.h"
 
 namespace ios {
@@ -24,7 +29,12 @@ namespace {
 constexpr int kWavesT = 8, kThreadsT = 64 * kWavesT;
 constexpr int kStagesT = 3;              // tiles of a wave's ring
 constexpr int kStepTiles = kWavesT;      // tiles of a step: one a wave
-// Steps that a block of rows costs beside its keys, the fewest of a share, and the keys from which blocks are cut.
+// Steps that a block of rows costs beside its keys (us for 1, 3 and 6: one sequence of 131072 tokens 80.5, 75.8, 76.4, the maps
+// in f16 29.8, 31.0, 35.3, in bf16 26.4, 25.9, 28.4); the fewest of a share (for 1, 3 and 6: the maps 30.9, 31.0, 34.3, one
+// sequence of 3100 tokens under 13 drafts 16.6, 19.9, 22.2, one of 20000 under 4 16.4, 16.9, 18.5, the others the same); and the
+// keys from which blocks are cut, so that there is a second launch (whole and cut: one sequence of 600 keys in float32 16.0 and
+// 18.7, 1000 21.1 and 20.7, 1300 24.6 and 20.7, in bf16 1000 13.4 and 16.7, 2000 17.3 and 18.0; 16 sequences of 300 21.4 and
+// 23.1, 600 25.1 and 23.0, 1000 30.9 and 26.9).  The maps: 16 sequences of 1 to 3100 tokens under 0 to 64 drafts of 16 heads.
 constexpr int kItemSteps = 3, kShareSteps = 3, kOneTree = 1024;
 
 // How the products over the cache are computed, for results in T:
@@ -39,8 +49,9 @@ template <class T> constexpr int kQueryParts = std::is_same_v<T, float> ? 3 : 1;
 
 // The largest weight is 2^kTopTree when its row's reference is set, and the reference is set anew when one would pass 2^6
 // times that: rows whose largest score grows by less than 6 (base 2) from the first tile on, which are nearly all, keep the
-// first.  A 16-bit weight is off by at most 2^-25, so 2^-34 of the largest: 10^6 keys together by 2^-14.  Float32's need no
-// such room, and scores near the reference are the more exact the nearer they are.
+// first.  A 16-bit weight is off by at most 2^-25, so 2^-34 of the largest: 10^6 keys together by 2^-14 (2^-38 in single-token
+// attention, whose rows follow their largest score sooner).  Float32's need no such room, and scores near the reference are the
+// more exact the nearer they are.
 template <class T> constexpr float kTopTree = std::is_same_v<T, float> ? 0.f : 9.f;
 template <class T> constexpr float kFarTree = kTopTree<T> + 6.f;
 
@@ -830,9 +841,9 @@ int64_t steps_of(const ios_attn_desc &d, int64_t q_tokens, int most, int w) {
 }
 
 // 16-row groups of a block.  Four read the cache once for 64 rows, but each wave then begins and ends with twice the work of
-// two: 32 sequences under 64 rows each 285 us against 371 (bf16; f16 532 against 574), one under 256 rows 77 against 83, but
-// maps of 1 to 3100 tokens 36 against 31 (f16 44 against 37).  So four where every workgroup has 12 steps; float32's three
-// parts of the queries and weights leave registers for two.
+// two: 32 sequences under 64 rows each 286 us against 370 (bf16; f16 530 against 578), one under 256 rows 76 against 78.5
+// (f16 121 against 122), but maps of 1 to 3100 tokens 32.3 against 25.9 (f16 38.6 against 31.0).  So four where every workgroup
+// has 12 steps; float32's three parts of the queries and weights leave registers for two.
 int row_groups(const ios_attn_desc &d, int64_t q_tokens, int most) {
   const int rows = most * (d.heads / d.kv_heads);
   if (rows <= 16) return 1;
@@ -861,7 +872,9 @@ hipError_t run(const Call &x) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !x.groups) return e;
   const int64_t rows = x.q.tokens * d.heads, parts = 2 * (int64_t)x.groups;
-  if (parts * W <= 16 * rows)                                     // few parts of a row: a wave for each, always from 2048 rows on
+  // A wave for each row where it has few parts (a wave and a workgroup each: the maps in bf16 25.9 and 29.9 us, 32 long
+  // sequences 284 and 299, but one of 131072 tokens under a single draft 28.3 and 23.5); always from 2048 rows on.
+  if (parts * W <= 16 * rows)
     hipLaunchKernelGGL((attn_tree_join_kernel<T, G, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, x.s, d.heads, ratio,
                        d.seqs, x.most, W, parts, x.out, x.lse, x.cu, x.part);
   else

@@ -8,7 +8,8 @@
 // us (190 MB, 52 .. 66 if the input stays in the 256 MB cache: the quantiser's
 // vector instructions, 66 per cent busy).  32 single tokens 5.6 and 3.8 us, a
 // chain of dependent loads (offsets, slot, length, page, values).  With rotation, 19136 tokens of 8 heads of 64 and 16 of
-// queries: 50 us for 130 MB (queries 23, keys and values 27, 17 unturned: vector units 60 per cent busy); 32 single tokens 6.2.
+// queries: 50 us for 130 MB (queries 23, keys and values 27, 17 unturned: vector units 60 per cent busy; every head's workgroup
+// makes its own table of the tile's cosines), in float32 72; 32 single tokens 6.2.
 // Accepted drafts of 256 sequences, 2048 tiles: 12.6 us, the same chain; with a sequence's tiles beside each other 17, as every
 // other workgroup, and so half of the XCDs, had none.
 #include "rotary.h"

@@ -11,7 +11,9 @@
 //
 // A chain of loads and sums, each of a few hundred nanoseconds: the walk (offsets, tree, probabilities), the row, its sum
 // across the card, the share that holds the mark.  32 chains over 131072 tokens, float32: 21 us (4 for the walk, 17 for 34 MB
-// of rows, which memory alone would take 7 for); one tree over 32003 tokens 10.
+// of rows, which memory alone would take 7 for); one tree over 32003 tokens 10.  A row that is read during the walk is read by
+// the walk's one workgroup: where three drafts behind the root fall one after the other, two such rows, 1, 8 and 32 sequences of
+// 131072 tokens take 58, 59 and 67 us in float32 (71, 71 and 78 in bf16) against 13, 14 and 19 where one falls.
 #include <type_traits>
 
 #include "decoder.h"
